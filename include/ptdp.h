@@ -455,6 +455,64 @@ int ptdp_attn_form(int kernel, int causal, int masked, int s, int b, int heads, 
  * dQ, which computes delta, and then dK/dV.  *split = 1: dK and dV are computed by waves of their own.  Returns as ptdp_attn_form. */
 int ptdp_attn_bwd_launch(int causal, int masked, int s, int b, int heads, int dh, int* together, int* split);
 
+/* ------------------------------------------------ parts of later GPT-style layers */
+/* Operators that take the place of one part of the layer above, as single kernels: rotary positions behind the QKV product instead
+ * of the position table, attention under spans, and the gated feed-forward block's fused products.  Conventions as everywhere: dev
+ * pointers, activations [s, b, width], no allocation, no synchronisation, capturable.  A row of qkv is [Q of `heads` heads | K of
+ * `kv_heads` | V of `kv_heads`], each head's dh columns contiguous; query head e uses key/value head e / (heads / kv_heads).
+ * heads % kv_heads == 0, dh % 8 == 0, dh <= 256.  s, b or rows of 0 are allowed and do nothing. */
+
+/* A head's first rot elements (rot % 8 == 0, 0 < rot <= dh) are rot / 2 pairs: element i with i + rot / 2 (HALVES), or neighbours 2 i, 2 i + 1. */
+enum { PTDP_ROTARY_HALVES = 0, PTDP_ROTARY_PAIRS = 1 };
+/* How a pair's frequency f = base^(-2 i / rot) / (2 pi), in turns per position, is scaled for contexts longer than the trained one:
+ *   PLAIN   f (factor, trained, slow, fast are not used)
+ *   LINEAR  f / factor
+ *   BASE    the base becomes base * factor^(rot / (rot - 2)); rot > 2
+ *   RAMP    by the turns r = trained * f that a pair makes over the trained length: r <= slow as LINEAR, r >= fast as PLAIN, between
+ *           them f (g + (1 - g) / factor) with g = (r - slow) / (fast - slow) */
+enum { PTDP_ROTARY_PLAIN = 0, PTDP_ROTARY_LINEAR, PTDP_ROTARY_BASE, PTDP_ROTARY_RAMP };
+/* Host only: the rot / 2 frequencies, to be copied to the device by the caller.  base, factor and trained in 1e-30 .. 1e30, 0 <= slow < fast <= 1e30,
+ * as far as `scaling` uses them; turns: host, rot / 2 doubles. */
+int ptdp_rotary_turns(int rot, double base, int scaling, double factor, double trained, double slow, double fast, double* turns);
+/* out = qkv with the pairs of every Q and K head turned by positions[i, j] * turns (in 64 bits, so any position) and multiplied by amplitude:
+ * (x, y) -> amplitude (x cos - y sin, x sin + y cos); the rest of the heads and V as they are.  qkv, out: [s, b, (heads + 2 kv_heads) dh] in
+ * `dtype`, the same buffer or two that do not overlap (in place, only what is rotated is read and written).  positions: int32 [s, b], any values,
+ * or NULL: the token index i.  turns: dev, rot / 2 doubles.  amplitude: finite. */
+int ptdp_rotary_fwd(int dtype, int layout, const void* qkv, const int32_t* positions, const double* turns, void* out, int s, int b, int heads,
+                    int kv_heads, int dh, int rot, float amplitude, void* stream);
+/* Its backward, gradients in place of the rows: the transposed map (the rotation by the negative angle, times amplitude). */
+int ptdp_rotary_bwd(int dtype, int layout, const void* dout, const int32_t* positions, const double* turns, void* dqkv, int s, int b, int heads,
+                    int kv_heads, int dh, int rot, float amplitude, void* stream);
+
+/* Spans: which keys a query sees, one interval for each query, built once per batch for all layers and both directions.
+ *   documents: int32 [s, b] or NULL (a sample is one document).  A document is a run of equal ids along i; a query sees only keys of its own
+ *     document.  Negative ids are padding: such a token sees nothing and is seen by none.
+ *   causal: 1: keys up to the query itself.  0: the whole document.
+ *   prefix: int32 [s, b] or NULL, with causal = 1 and window = 0 only: the entry of a document's first token (the others are not read) is the number of
+ *     the document's first tokens that all of its tokens see (limited to 0 .. its length).
+ *   window: 0, or only keys less than `window` tokens away.
+ * spans: dev, ptdp_attn_spans_bytes(s, b) bytes, 16-byte aligned. */
+size_t ptdp_attn_spans_bytes(int s, int b);
+int ptdp_attn_spans(int causal, int window, const int32_t* documents, const int32_t* prefix, void* spans, int s, int b, void* stream);
+
+/* struct_size must be sizeof(ptdp_attn_span_cfg).  scale: of q.k, 1e-10 .. 1e10.  cap: 0 (none) or 1e-3 .. 1e10: scaled scores become
+ * cap tanh(score / cap).  bf16: dh in {32, 64, 96, 128, 160}, else PTDP_E_UNSUPPORTED; so are row pitches b (heads + 2 kv_heads) dh of about 143
+ * million elements and more (fp32: 2^31, heads or b beyond 65535). */
+typedef struct ptdp_attn_span_cfg {
+  uint32_t struct_size;
+  int32_t s, b, heads, kv_heads, dh, dtype;
+  float scale, cap;
+} ptdp_attn_span_cfg;
+/* ctx = softmax over the span's keys of (capped, scaled q.k) - slopes[e] |i - k|, times V; lse of those scores.  spans: as built for this s, b, or
+ * NULL: the causal mask over whole samples.  slopes: fp32 [heads] or NULL (constants: no gradient).  ctx [s, b, heads dh], lse [b, heads, s] fp32.
+ * A query with an empty span gets zeros and lse = -inf.  What a query does not see reaches none of its results, infinities and NaN included. */
+int ptdp_attn_span_fwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, void* ctx, float* lse, void* stream);
+/* dqkv (all of it; not qkv's buffer) from dctx; K and V gradients are summed over the heads that share them, without atomics.  workspace: dev,
+ * ptdp_attn_span_workspace_bytes(cfg) bytes (0 on an invalid cfg). */
+int ptdp_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, const void* ctx, const float* lse,
+                       const void* dctx, void* dqkv, void* workspace, void* stream);
+size_t ptdp_attn_span_workspace_bytes(const ptdp_attn_span_cfg* cfg);
+
 /* ---------------------------------------------------------------- ceilings */
 /* What the chip is seen to do, for reading roofline fractions: a loop of
  * v_mfma_f32_32x32x16_bf16 on registers only (workgroups x 8 waves x 8

@@ -25,6 +25,8 @@ OK, E_INVALID_ARG, E_UNSUPPORTED, E_NULL_PTR, E_TOO_SMALL, E_HIP, E_STATE = 0, -
 F32, BF16 = 0, 1
 GELU_ERF, GELU_TANH = 0, 1
 GEMM_NN, GEMM_NT, GEMM_TN = 0, 1, 2
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_RAMP = 0, 1, 2, 3
 STASH_FIELDS = ("X", "U", "QKV", "CTX", "X1", "U2", "Z", "G", "MU1", "RSTD1", "MU2", "RSTD2", "LSE")
 WS_FIELDS = ("DO", "DU", "DX1", "CHAIN", "DZ", "DCTX", "DQKV", "DMO")
 PARAM_NAMES = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o", "ln2_g", "ln2_b", "w_1", "b_1", "w_2", "b_2")
@@ -55,6 +57,11 @@ class Step(C.Structure):
     _fields_ = [("kind", C.c_int32), ("chunk", C.c_int32), ("microbatch", C.c_int32)]
 
 
+class AttnSpanCfg(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("s", C.c_int32), ("b", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("dh", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("cap", C.c_float)]
+
+
 class ProfEntry(C.Structure):
     _fields_ = [("ms", C.c_double), ("work", C.c_double), ("launches", C.c_int64)]
 
@@ -63,8 +70,15 @@ def make_cfg(h, a, t, s, b, dtype=BF16, p_hidden=0.0, ln_eps=1e-5, seed=0, gelu_
     return LayerCfg(C.sizeof(LayerCfg), h, a, t, s, b, dtype, causal, gelu_mode, p_hidden, ln_eps, seed)
 
 
+def make_span_cfg(s, b, heads, kv_heads, dh, dtype=BF16, scale=None, cap=0.0):
+    """scale None: 1 / sqrt(dh)."""
+    return AttnSpanCfg(C.sizeof(AttnSpanCfg), s, b, heads, kv_heads, dh, dtype, dh ** -0.5 if scale is None else scale, cap)
+
+
 _vp, _i, _i64, _u64, _u32, _f, _sz = C.c_void_p, C.c_int, C.c_int64, C.c_uint64, C.c_uint32, C.c_float, C.c_size_t
+_d = C.c_double
 _cfgp = C.POINTER(LayerCfg)
+_spanp = C.POINTER(AttnSpanCfg)
 
 # name -> (restype, argtypes); one entry per declaration in include/ptdp.h
 SIGNATURES = {
@@ -124,6 +138,14 @@ SIGNATURES = {
     "ptdp_attn_masked_fwd": (_i, [_i, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp]),
     "ptdp_attn_masked_bwd": (_i, [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp]),
     "ptdp_chunk_set_mask": (_i, [_vp, _vp]),
+    "ptdp_rotary_turns": (_i, [_i, _d, _i, _d, _d, _d, _d, C.POINTER(_d)]),
+    "ptdp_rotary_fwd": (_i, [_i, _i, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _f, _vp]),
+    "ptdp_rotary_bwd": (_i, [_i, _i, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _f, _vp]),
+    "ptdp_attn_spans_bytes": (_sz, [_i, _i]),
+    "ptdp_attn_spans": (_i, [_i, _i, _vp, _vp, _vp, _i, _i, _vp]),
+    "ptdp_attn_span_workspace_bytes": (_sz, [_spanp]),
+    "ptdp_attn_span_fwd": (_i, [_spanp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "ptdp_attn_span_bwd": (_i, [_spanp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "ptdp_ceiling_mfma": (_i, [_vp, _i, _i, _i, C.POINTER(C.c_double), _vp]),
     "ptdp_ceiling_copy": (_i, [_vp, _vp, _sz, _vp]),
     "ptdp_prof_enable": (_i, [_i]),
@@ -230,6 +252,13 @@ def stash_offsets(cfg):
 
 def workspace_offsets(cfg):
     return {name: lib.ptdp_workspace_offset(C.byref(cfg), i) for i, name in enumerate(WS_FIELDS)}
+
+
+def rotary_turns(rot, base=10000.0, scaling=ROTARY_PLAIN, factor=1.0, trained=1.0, slow=0.0, fast=1.0):
+    """The rot / 2 frequencies in turns per position, as a list."""
+    turns = (_d * max(0, rot // 2))()
+    check(lib.ptdp_rotary_turns(rot, base, scaling, factor, trained, slow, fast, turns), "rotary_turns")
+    return list(turns)
 
 
 def prof_collect():

@@ -950,6 +950,103 @@ int ptdp_attn_masked_bwd(int dtype, const void* qkv, const uint8_t* mask, const 
   return launch_attn_bwd(dtype, qkv, ctx, lse, dctx, dqkv, delta, s, b, heads, dh, mask, 0, (hipStream_t)stream);
 }
 
+// ------------------------------------------------------------------------- parts of later GPT-style layers
+// Here the 16-byte alignment of device buffers is checked (null passes).
+}  // extern "C"
+template <class... P> static int check_aligned(const P*... p) {
+  return ((0 | ... | reinterpret_cast<uintptr_t>(p)) & 15) == 0 ? PTDP_OK : PTDP_E_INVALID_ARG;
+}
+extern "C" {
+static int check_heads(int heads, int kv_heads, int dh) {
+  if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || dh <= 0 || dh % 8 != 0 || dh > 256) return PTDP_E_INVALID_ARG;
+  return (int64_t)heads + 2ll * kv_heads > 0x7fffffffll / dh ? PTDP_E_UNSUPPORTED : PTDP_OK;   // a row's length is an int
+}
+static bool within(double x, double lo, double hi) { return x >= lo && x <= hi; }   // false for NaN
+
+int ptdp_rotary_turns(int rot, double base, int scaling, double factor, double trained, double slow, double fast, double* turns) {
+  if (rot <= 0 || rot % 8 != 0 || rot > 256 || scaling < PTDP_ROTARY_PLAIN || scaling > PTDP_ROTARY_RAMP) return PTDP_E_INVALID_ARG;
+  const double tiny = 1e-30, huge = 1e30;
+  if (!within(base, tiny, huge) || (scaling != PTDP_ROTARY_PLAIN && !within(factor, tiny, huge))) return PTDP_E_INVALID_ARG;
+  if (scaling == PTDP_ROTARY_RAMP && (!within(trained, tiny, huge) || !within(slow, 0.0, huge) || !within(fast, 0.0, huge) || !(slow < fast)))
+    return PTDP_E_INVALID_ARG;
+  if (!turns) return PTDP_E_NULL_PTR;
+  if (scaling == PTDP_ROTARY_BASE) base *= std::pow(factor, (double)rot / (rot - 2));
+  for (int i = 0; i < rot / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rot) / 6.283185307179586477;
+    if (scaling == PTDP_ROTARY_LINEAR) f /= factor;
+    if (scaling == PTDP_ROTARY_RAMP) {
+      const double r = trained * f, g = r <= slow ? 0.0 : r >= fast ? 1.0 : (r - slow) / (fast - slow);
+      f *= g + (1.0 - g) / factor;
+    }
+    turns[i] = f;
+  }
+  return PTDP_OK;
+}
+
+static int rotary(int dtype, int layout, const void* in, const int32_t* positions, const double* turns, void* out, int s, int b, int heads, int kv_heads,
+                  int dh, int rot, float amplitude, bool back, void* stream) {
+  PTDP_TRY(check_dtype(dtype));
+  PTDP_TRY(check_heads(heads, kv_heads, dh));
+  if (layout != PTDP_ROTARY_HALVES && layout != PTDP_ROTARY_PAIRS) return PTDP_E_INVALID_ARG;
+  if (s < 0 || b < 0 || rot <= 0 || rot > dh || rot % 8 != 0 || !std::isfinite(amplitude)) return PTDP_E_INVALID_ARG;
+  if ((int64_t)s * b > 0x7fffffffll) return PTDP_E_UNSUPPORTED;
+  if (!in || !turns || !out) return PTDP_E_NULL_PTR;
+  PTDP_TRY(check_aligned(in, turns, out));
+  if (s == 0 || b == 0) return PTDP_OK;
+  return launch_rotary(dtype, layout, in, positions, turns, out, s, b, heads, kv_heads, dh, rot, amplitude, back, (hipStream_t)stream);
+}
+int ptdp_rotary_fwd(int dtype, int layout, const void* qkv, const int32_t* positions, const double* turns, void* out, int s, int b, int heads,
+                    int kv_heads, int dh, int rot, float amplitude, void* stream) {
+  return rotary(dtype, layout, qkv, positions, turns, out, s, b, heads, kv_heads, dh, rot, amplitude, false, stream);
+}
+int ptdp_rotary_bwd(int dtype, int layout, const void* dout, const int32_t* positions, const double* turns, void* dqkv, int s, int b, int heads,
+                    int kv_heads, int dh, int rot, float amplitude, void* stream) {
+  return rotary(dtype, layout, dout, positions, turns, dqkv, s, b, heads, kv_heads, dh, rot, amplitude, true, stream);
+}
+
+static int check_spans(int s, int b) {
+  if (s < 0 || b < 0) return PTDP_E_INVALID_ARG;
+  return b > 65535 || s > 0x7fffffff - 65536 ? PTDP_E_UNSUPPORTED : PTDP_OK;
+}
+size_t ptdp_attn_spans_bytes(int s, int b) { return check_spans(s, b) == PTDP_OK ? attn_spans_bytes(s, b) : 0; }
+int ptdp_attn_spans(int causal, int window, const int32_t* documents, const int32_t* prefix, void* spans, int s, int b, void* stream) {
+  if ((causal != 0 && causal != 1) || window < 0 || (prefix && (!causal || window > 0))) return PTDP_E_INVALID_ARG;
+  PTDP_TRY(check_spans(s, b));
+  if (!spans) return PTDP_E_NULL_PTR;
+  PTDP_TRY(check_aligned(spans));
+  if (s == 0 || b == 0) return PTDP_OK;
+  return launch_attn_spans(causal, window, documents, prefix, spans, s, b, (hipStream_t)stream);
+}
+
+static int check_span_cfg(const ptdp_attn_span_cfg* c) {
+  if (!c) return PTDP_E_NULL_PTR;
+  if (c->struct_size != sizeof(ptdp_attn_span_cfg)) return PTDP_E_INVALID_ARG;
+  PTDP_TRY(check_dtype(c->dtype));
+  PTDP_TRY(check_heads(c->heads, c->kv_heads, c->dh));
+  if (!within(c->scale, 1e-10, 1e10) || !(c->cap == 0.f || within(c->cap, 1e-3, 1e10))) return PTDP_E_INVALID_ARG;
+  PTDP_TRY(check_spans(c->s, c->b));
+  return attn_dh_supported(c->dtype, c->dh) && attn_span_fits(c) ? PTDP_OK : PTDP_E_UNSUPPORTED;
+}
+size_t ptdp_attn_span_workspace_bytes(const ptdp_attn_span_cfg* cfg) {
+  return check_span_cfg(cfg) == PTDP_OK ? align256((size_t)cfg->b * cfg->heads * cfg->s * sizeof(float)) : 0;
+}
+int ptdp_attn_span_fwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, void* ctx, float* lse, void* stream) {
+  PTDP_TRY(check_span_cfg(cfg));
+  if (!qkv || !ctx || !lse) return PTDP_E_NULL_PTR;
+  PTDP_TRY(check_aligned(qkv, spans, ctx));
+  if (cfg->s == 0 || cfg->b == 0) return PTDP_OK;
+  return launch_attn_span_fwd(cfg, qkv, spans, slopes, ctx, lse, (hipStream_t)stream);
+}
+int ptdp_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, const void* ctx, const float* lse,
+                       const void* dctx, void* dqkv, void* workspace, void* stream) {
+  PTDP_TRY(check_span_cfg(cfg));
+  if (!qkv || !ctx || !lse || !dctx || !dqkv || !workspace) return PTDP_E_NULL_PTR;
+  if (dqkv == qkv) return PTDP_E_INVALID_ARG;
+  PTDP_TRY(check_aligned(qkv, spans, ctx, dctx, dqkv, workspace));
+  if (cfg->s == 0 || cfg->b == 0) return PTDP_OK;
+  return launch_attn_span_bwd(cfg, qkv, spans, slopes, ctx, lse, dctx, dqkv, (float*)workspace, (hipStream_t)stream);
+}
+
 // ----------------------------------------------------------------------------------- profiling
 int ptdp_prof_enable(int on) {
   std::lock_guard<std::mutex> lock(g_prof_mu);

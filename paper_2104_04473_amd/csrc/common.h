@@ -255,5 +255,14 @@ int launch_embed_fwd(int dtype, const int32_t* tokens, const void* e_word, const
 int launch_embed_bwd(int dtype, const int32_t* tokens, const void* dx, float* d_e_word, float* d_e_pos, int s, int b, int h, int v0, int vrows, float p, uint64_t key, hipStream_t st);
 int launch_xent(int dtype, void* logits, const int32_t* targets, float* token_loss, float* loss, int rows, int vrows,
                 int v0, float grad_scale, hipStream_t st);
+// parts of later GPT-style layers (rotary.hip, attn_span.hip)
+int launch_rotary(int dtype, int layout, const void* qkv, const int32_t* positions, const double* turns, void* out, int s, int b, int heads,
+                  int kv_heads, int dh, int rot, float amplitude, bool back, hipStream_t st);
+size_t attn_spans_bytes(int s, int b);
+int launch_attn_spans(int causal, int window, const int32_t* documents, const int32_t* prefix, void* spans, int s, int b, hipStream_t st);
+bool attn_span_fits(const ptdp_attn_span_cfg* cfg);   // a valid one's sizes: what the kernels can address and a launch can number
+int launch_attn_span_fwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, void* ctx, float* lse, hipStream_t st);
+int launch_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, const void* ctx, const float* lse,
+                         const void* dctx, void* dqkv, float* delta, hipStream_t st);
 
 }  // namespace ptdp
