@@ -513,6 +513,21 @@ int ptdp_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const voi
                        const void* dctx, void* dqkv, void* workspace, void* stream);
 size_t ptdp_attn_span_workspace_bytes(const ptdp_attn_span_cfg* cfg);
 
+/* Gated feed-forward block, y = g w_2 with g = f(z_gate + b_gate) (z_up + b_up) and z = u w, the columns of w [width, 2 inner] (and of z, bias) ordered
+ * [gate | up].  f: SILU a / (1 + exp(-a)), the two GELUs of ptdp_layer_cfg, SIGMOID or RELU (derivative 0 at 0). */
+enum { PTDP_GATE_SILU = 0, PTDP_GATE_GELU_ERF, PTDP_GATE_GELU_TANH, PTDP_GATE_SIGMOID, PTDP_GATE_RELU };
+/* z [rows, 2 inner] (before the bias, what the backward wants) and g [rows, inner] from u [rows, width]: both projections, activation and product; bf16:
+ * in one kernel, g from the unrounded sums.  bias [2 inner] or NULL.  width, inner multiples of 8.  PTDP_E_UNSUPPORTED: u or w of 2 GiB or more,
+ * rows of z of 8 MiB or more. */
+int ptdp_gated_mlp_fwd(int dtype, int gate, const void* u, const void* w, const void* bias, void* z, void* g, int rows, int width, int inner,
+                       void* stream);
+/* dz [rows, 2 inner] (may be z's buffer) = the gradient of z + bias from dy [rows, width] through dg = dy w_2^T, w_2 [inner, width]; dbias [2 inner] fp32 +=
+ * its column sums (NULL: none).  The block's other gradients are plain products: w_2 += g^T dy, w += u^T dz, du = dz w^T (ptdp_gemm).
+ * workspace: dev, ptdp_gated_mlp_workspace_bytes bytes (0 where the sizes are refused). */
+int ptdp_gated_mlp_bwd(int dtype, int gate, const void* dy, const void* w2, const void* z, const void* bias, void* dz, float* dbias, void* workspace,
+                       int rows, int width, int inner, void* stream);
+size_t ptdp_gated_mlp_workspace_bytes(int dtype, int rows, int width, int inner);
+
 /* ---------------------------------------------------------------- ceilings */
 /* What the chip is seen to do, for reading roofline fractions: a loop of
  * v_mfma_f32_32x32x16_bf16 on registers only (workgroups x 8 waves x 8

@@ -25,6 +25,7 @@ OK, E_INVALID_ARG, E_UNSUPPORTED, E_NULL_PTR, E_TOO_SMALL, E_HIP, E_STATE = 0, -
 F32, BF16 = 0, 1
 GELU_ERF, GELU_TANH = 0, 1
 GEMM_NN, GEMM_NT, GEMM_TN = 0, 1, 2
+GATE_SILU, GATE_GELU_ERF, GATE_GELU_TANH, GATE_SIGMOID, GATE_RELU = 0, 1, 2, 3, 4
 ROTARY_HALVES, ROTARY_PAIRS = 0, 1
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_RAMP = 0, 1, 2, 3
 STASH_FIELDS = ("X", "U", "QKV", "CTX", "X1", "U2", "Z", "G", "MU1", "RSTD1", "MU2", "RSTD2", "LSE")
@@ -146,6 +147,9 @@ SIGNATURES = {
     "ptdp_attn_span_workspace_bytes": (_sz, [_spanp]),
     "ptdp_attn_span_fwd": (_i, [_spanp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "ptdp_attn_span_bwd": (_i, [_spanp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "ptdp_gated_mlp_fwd": (_i, [_i, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp]),
+    "ptdp_gated_mlp_bwd": (_i, [_i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp]),
+    "ptdp_gated_mlp_workspace_bytes": (_sz, [_i, _i, _i, _i]),
     "ptdp_ceiling_mfma": (_i, [_vp, _i, _i, _i, C.POINTER(C.c_double), _vp]),
     "ptdp_ceiling_copy": (_i, [_vp, _vp, _sz, _vp]),
     "ptdp_prof_enable": (_i, [_i]),

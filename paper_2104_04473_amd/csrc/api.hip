@@ -1047,6 +1047,31 @@ int ptdp_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const voi
   return launch_attn_span_bwd(cfg, qkv, spans, slopes, ctx, lse, dctx, dqkv, (float*)workspace, (hipStream_t)stream);
 }
 
+static int check_gated(int dtype, int gate, int rows, int width, int inner) {
+  PTDP_TRY(check_rw(dtype, rows, width));
+  if (inner <= 0 || inner % 8 != 0 || gate < PTDP_GATE_SILU || gate > PTDP_GATE_RELU) return PTDP_E_INVALID_ARG;
+  return gated_mlp_fits(dtype, rows, width, inner) ? PTDP_OK : PTDP_E_UNSUPPORTED;
+}
+size_t ptdp_gated_mlp_workspace_bytes(int dtype, int rows, int width, int inner) {
+  return check_gated(dtype, PTDP_GATE_SILU, rows, width, inner) == PTDP_OK ? gated_mlp_workspace_bytes(dtype, rows, width, inner) : 0;
+}
+int ptdp_gated_mlp_fwd(int dtype, int gate, const void* u, const void* w, const void* bias, void* z, void* g, int rows, int width, int inner,
+                       void* stream) {
+  PTDP_TRY(check_gated(dtype, gate, rows, width, inner));
+  if (!u || !w || !z || !g) return PTDP_E_NULL_PTR;
+  PTDP_TRY(check_aligned(u, w, bias, z, g));
+  if (rows == 0) return PTDP_OK;
+  return launch_gated_mlp_fwd(dtype, gate, u, w, bias, z, g, rows, width, inner, (hipStream_t)stream);
+}
+int ptdp_gated_mlp_bwd(int dtype, int gate, const void* dy, const void* w2, const void* z, const void* bias, void* dz, float* dbias, void* workspace,
+                       int rows, int width, int inner, void* stream) {
+  PTDP_TRY(check_gated(dtype, gate, rows, width, inner));
+  if (!dy || !w2 || !z || !dz || !workspace) return PTDP_E_NULL_PTR;
+  PTDP_TRY(check_aligned(dy, w2, bias, z, dz, dbias, workspace));
+  if (rows == 0) return PTDP_OK;
+  return launch_gated_mlp_bwd(dtype, gate, dy, w2, z, bias, dz, dbias, workspace, rows, width, inner, (hipStream_t)stream);
+}
+
 // ----------------------------------------------------------------------------------- profiling
 int ptdp_prof_enable(int on) {
   std::lock_guard<std::mutex> lock(g_prof_mu);

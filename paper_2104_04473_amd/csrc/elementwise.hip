@@ -3,7 +3,7 @@
 // All of them move 16 bytes per lane per access, keep fp32 arithmetic, and reduce with wavefront
 // shuffles; column sums (bias / LayerNorm parameter gradients) are two-stage and deterministic.
 #include "colsum.h"
-#include "gelu.h"
+#include "gate.h"
 
 namespace ptdp {
 
@@ -642,6 +642,94 @@ bias_gelu_bwd_kernel(const T* dg, const T* __restrict__ z, const T* __restrict__
 }
 
 // ------------------------------------------------------------------------------------------------
+// Gated feed-forward block in fp32 (bf16: in the products' output stages): rows of z (and dz) are [gate | up], 2 * inner long.
+// ------------------------------------------------------------------------------------------------
+template <int GATE>
+__global__ void gated_fwd_rows_kernel(const float* __restrict__ z, const float* __restrict__ bias, float* __restrict__ g, size_t total_vec, int nvec_row) {
+  constexpr int N = 4;
+  for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < total_vec; i += (size_t)gridDim.x * blockDim.x) {
+    const size_t r = i / nvec_row, c = i % nvec_row;
+    Vec16<float> v;
+    float a[N], u[N], ba[N], bu[N];
+    v.load(z + (2 * r * nvec_row + c) * N);
+    v.unpack(a);
+    v.load(z + ((2 * r + 1) * nvec_row + c) * N);
+    v.unpack(u);
+#pragma unroll
+    for (int j = 0; j < N; ++j) ba[j] = bu[j] = 0.f;
+    if (bias) {
+      v.load(bias + c * N);
+      v.unpack(ba);
+      v.load(bias + (nvec_row + c) * N);
+      v.unpack(bu);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) a[j] = gate_f<GATE>(a[j] + ba[j]) * (u[j] + bu[j]);
+    v.pack(a);
+    v.store(g + i * N);
+  }
+}
+// as bias_gelu_bwd_kernel; the thread owns a column group of either half.  part null: no column sums
+template <int GATE>
+__global__ void __launch_bounds__(64 * kColLanes)
+gated_bwd_rows_kernel(const float* __restrict__ dg, const float* z, const float* __restrict__ bias, float* dz, float* __restrict__ part, int rows, int inner) {
+  constexpr int N = 4;
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63);
+  float sa[N], su[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) sa[j] = su[j] = 0.f;
+  if (c < inner / N) {
+    Vec16<float> v;
+    float ba[N], bu[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) ba[j] = bu[j] = 0.f;
+    if (bias) {
+      v.load(bias + (size_t)c * N);
+      v.unpack(ba);
+      v.load(bias + inner + (size_t)c * N);
+      v.unpack(bu);
+    }
+    const int r0 = blockIdx.y * kColRows + (threadIdx.x >> 6), r1 = min(rows, (int)(blockIdx.y + 1) * kColRows);
+#pragma unroll 1
+    for (int r = r0; r < r1; r += kColLanes) {
+      const size_t at = (size_t)r * 2 * inner + (size_t)c * N;
+      Vec16<float> va, vu;
+      float d[N], a[N], u[N];
+      v.load(dg + (size_t)r * inner + (size_t)c * N);
+      va.load(z + at);
+      vu.load(z + at + inner);
+      v.unpack(d);
+      va.unpack(a);
+      vu.unpack(u);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        float df;
+        const float f = gate_grad_f<GATE>(a[j] + ba[j], &df);
+        a[j] = d[j] * df * (u[j] + bu[j]);
+        u[j] = d[j] * f;
+        sa[j] += a[j];
+        su[j] += u[j];
+      }
+      va.pack(a);
+      vu.pack(u);
+      va.store(dz + at);
+      vu.store(dz + at + inner);
+    }
+  }
+  if (!part) return;
+  __shared__ __attribute__((aligned(16))) float red[kColLanes][64 * N];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, t = threadIdx.x, col = blockIdx.x * 64 * N + t;   // one column a thread
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (h) __syncthreads();   // the first half's sums have been read
+#pragma unroll
+    for (int j = 0; j < N; ++j) red[w][lane * N + j] = h ? su[j] : sa[j];
+    __syncthreads();
+    if (t < 64 * N && col < inner) part[(size_t)blockIdx.y * 2 * inner + h * inner + col] = colsum_lanes_sum<N>(red, t);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
 // bias + dropout + add
 // ------------------------------------------------------------------------------------------------
 template <typename T>
@@ -1013,6 +1101,27 @@ int launch_bias_gelu_bwd(int dtype, int mode, const void* dg, const void* z, con
   if (rows == 0) return PTDP_OK;
   return dtype == PTDP_BF16 ? gelu_bwd_t<bf16_t>(mode, dg, z, bias, dz, dbias, scratch, rows, width, st, defer)
                             : gelu_bwd_t<float>(mode, dg, z, bias, dz, dbias, scratch, rows, width, st, defer);
+}
+
+// g = f(z_gate + b) (z_up + b) of fp32 rows
+int launch_gated_act(int gate, const float* z, const float* bias, float* g, int rows, int inner, hipStream_t st) {
+  Launch L(PTDP_K_GELU_FWD, (double)rows * inner * 12, st);
+  const size_t total = (size_t)rows * inner / 4;
+  with_gate(gate, [&](auto kind) {
+    hipLaunchKernelGGL((gated_fwd_rows_kernel<decltype(kind)::value>), dim3(stream_grid(total)), dim3(256), 0, st, z, bias, g, total, inner / 4);
+  });
+  return L.status();
+}
+// dz from dg (dz may be z), *parts rows of partial column sums to part (or null)
+int launch_gated_act_bwd(int gate, const float* dg, const float* z, const float* bias, float* dz, float* part, int rows, int inner, int* parts,
+                         hipStream_t st) {
+  const dim3 grid = colsum_grid(inner / 4, rows);
+  *parts = grid.y;
+  Launch L(PTDP_K_GELU_BWD, (double)rows * inner * 20, st);
+  with_gate(gate, [&](auto kind) {
+    hipLaunchKernelGGL((gated_bwd_rows_kernel<decltype(kind)::value>), grid, dim3(64 * kColLanes), 0, st, dg, z, bias, dz, part, rows, inner);
+  });
+  return L.status();
 }
 
 template <typename T>

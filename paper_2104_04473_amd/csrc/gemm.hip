@@ -11,7 +11,7 @@
 // into MFMA fragments by transposing LDS reads.
 // fp32 path: v_mfma_f32_32x32x2_f32, operands straight from memory (small configurations).
 #include "colsum.h"
-#include "gelu.h"
+#include "gate.h"
 #include <type_traits>
 
 namespace ptdp {
@@ -58,7 +58,8 @@ constexpr int f32_most_waves(int nb) { return nb == 1 ? 8 : 4; }   // waves that
 // What an output stage does beside writing C.  EPI_GELU (NN): C = A B and g = GeLU(C + b).  EPI_GELU_GRAD (NT): C = (A B^T) * GeLU'(z + b), and
 // the column sums of C over blocks of rows to part[block][N].  Both from what a kernel of its own would read: the product as it is stored.
 // EPI_BDA (NN, bf16): C = z + Drop(A B + b), the residual sum behind the last layer's second MLP product.
-enum { EPI_PLAIN = 0, EPI_GELU = 1, EPI_GELU_GRAD = 2, EPI_BDA = 3 };
+// EPI_GATED (NN), EPI_GATED_GRAD (NT), bf16: the gated feed-forward block's, see gated_store and gated_grad_store.
+enum { EPI_PLAIN = 0, EPI_GELU = 1, EPI_GELU_GRAD = 2, EPI_BDA = 3, EPI_GATED = 4, EPI_GATED_GRAD = 5 };
 template <int KIND, int MODE = PTDP_GELU_ERF> struct Epi {   // MODE: PTDP_GELU_*
   static constexpr int kKind = KIND, kMode = MODE;
 };
@@ -494,8 +495,9 @@ template <bool KSLOW, int W = 128> struct HalfLoad {
   int kpos[2];         // k of the lane's chunk inside the k-tile
   bool plain;          // no offset above goes negative
 
-  // the descriptor's base is the block's first row (k-contiguous: base + row0*ld; k-slow: base + row0)
-  __device__ __forceinline__ void init(size_t ld, int rows_left, int wave, int lane) {
+  // the descriptor's base is the block's first row (k-contiguous: base + row0*ld; k-slow: base + row0).  GAP (k-slow): half 1 is not the next 128 rows
+  // but those `gap` rows further on, and rows_left counts either half's.
+  template <bool GAP = false> __device__ __forceinline__ void init(size_t ld, int rows_left, int wave, int lane, int gap = 128) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       if (!KSLOW) {
@@ -513,9 +515,9 @@ template <bool KSLOW, int W = 128> struct HalfLoad {
         kpos[i] = k;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int at = row_of_96(h, chunk * 8);
-          if (W == 128) off[h][i] = h * 128 + chunk * 8 < rows_left ? (uint32_t)(((size_t)k * ld + h * 128 + chunk * 8) * 2) - i * 1024u : kOob;
-          else off[h][i] = chunk * 8 < W && at < rows_left ? (uint32_t)(((size_t)k * ld + at) * 2) - i * 1024u : kOob;
+          const int at = GAP ? h * gap + chunk * 8 : row_of_96(h, chunk * 8);
+          if (W == 128) off[h][i] = (GAP ? 0 : h * 128) + chunk * 8 < rows_left ? (uint32_t)(((size_t)k * ld + h * gap + chunk * 8) * 2) - i * 1024u : kOob;
+          else off[h][i] = chunk * 8 < W && (GAP ? chunk * 8 : at) < rows_left ? (uint32_t)(((size_t)k * ld + at) * 2) - i * 1024u : kOob;
         }
       }
     }
@@ -616,8 +618,9 @@ template <int NS, int RB> __device__ __forceinline__ void zero_acc(StripAcc<NS, 
 // A half-tile is requested one phase after the phase in which every wave has finished reading its predecessor (two
 // tiles older, same place) and is read six phases later; the wait in front of that read leaves the ten younger loads
 // in flight (vmcnt counts loads in order), so the queue never drains inside the loop.
-template <bool TA, bool TB>
-__device__ __forceinline__ void gemm_mainloop(TileAcc& acc, const GemmArgs& g, int m0, int n0, int kt0, int kt1, char* smem) {
+// GAP: B's second half-tile is 128 columns `gap` further on (and g.N counts either half's columns).
+template <bool TA, bool TB, bool GAP = false>
+__device__ __forceinline__ void gemm_mainloop(TileAcc& acc, const GemmArgs& g, int m0, int n0, int kt0, int kt1, char* smem, int gap = 128) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;   // wave-uniform: LDS bases and M0 values stay in scalar registers
   // buffer descriptors start at the block's first row so that lane offsets stay small
   const bf16_t* a_base = TA ? g.A + m0 : g.A + (size_t)m0 * g.lda;
@@ -631,7 +634,7 @@ __device__ __forceinline__ void gemm_mainloop(TileAcc& acc, const GemmArgs& g, i
   HalfLoad<TA> la;
   HalfLoad<TB> lb;
   la.init(g.lda, g.M - m0, wave, lane);
-  lb.init(g.ldb, g.N - n0, wave, lane);
+  lb.template init<GAP>(g.ldb, g.N - n0, wave, lane, gap);
   FragRead<TA, 4> fa;
   FragRead<TB, 2> fb;
   fa.init(smem, (wave >> 2) * 64, lane);
@@ -959,6 +962,161 @@ __device__ __forceinline__ void gemm_epilogue(const StripAcc<NS, RB>& acc, const
   }
 }
 
+// The gated feed-forward block's products (bf16), rows of z: [gate | up], 2 * inner long.
+struct GatedArgs {
+  const bf16_t* bias;   // [2 inner] or null
+  bf16_t *z, *g;        // forward: z and g; backward: z is read, g is dz
+  float* part;          // backward: column sums over blocks of rows, [block][2 inner], or null
+  int inner, gate;
+};
+template <int N> __device__ __forceinline__ void load_bias(const bf16_t* bias, int c, int last, float (&f)[N]) {   // N values from c, at most from last
+  static_assert(N == 4 || N == 8);
+#pragma unroll
+  for (int j = 0; j < N; ++j) f[j] = 0.f;
+  if (!bias) return;
+#pragma unroll
+  for (int h = 0; h < N / 4; ++h) {
+    const uint2 w = *reinterpret_cast<const uint2*>(bias + min(c, last) + 4 * h);
+    f[4 * h] = __uint_as_float(w.x << 16); f[4 * h + 1] = __uint_as_float(w.x & 0xffff0000u);
+    f[4 * h + 2] = __uint_as_float(w.y << 16); f[4 * h + 3] = __uint_as_float(w.y & 0xffff0000u);
+  }
+}
+// Forward: z = the product, g = f(z_gate + b) (z_up + b) from the fp32 sums (g is rounded once; z's rounding does not enter it).  A lane has
+// gate and up of the same columns: in strips 2 p and 2 p + 1 (BNI inner columns to a tile, 32 to a pair of strips), or, one strip to a
+// wave, in the strip's two blocks of 16.  row, col: of pair p, col counted in inner columns.
+template <int GATE, int BM, int BNI, int NS, int RB>
+__device__ __forceinline__ void gated_store(const StripAcc<NS, RB>& acc, const int* row, const int* col, const GatedArgs& e, int M, int m0, int n0) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+  constexpr int NP = NS > 1 ? NS / 2 : 1;
+  const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4, F = e.inner, c8 = 16 * (q & 1) + 8 * (q >> 1);
+  const uint32_t zp = (uint32_t)F * 4, gp = (uint32_t)F * 2, rows = min(BM, M - m0) - 1, tail = min(BNI, F - n0) * 2;
+  bf16_t* z = e.z + (size_t)m0 * 2 * F + n0;
+  const auto rz = __builtin_amdgcn_make_buffer_rsrc(z, 0, rows * zp + tail, 0x00020000), ru = __builtin_amdgcn_make_buffer_rsrc(z + F, 0, rows * zp + tail, 0x00020000);
+  const auto rg = __builtin_amdgcn_make_buffer_rsrc(e.g + (size_t)m0 * F + n0, 0, rows * gp + tail, 0x00020000);
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    float bg[2][4], bu[2][4];
+#pragma unroll
+    for (int j = 0; j < (NS > 1 ? 2 : 1); ++j) {
+      load_bias<4>(e.bias, n0 + col[p] + j * 16 + 4 * q, F - 4, bg[j]);
+      load_bias<4>(e.bias ? e.bias + F : nullptr, n0 + col[p] + j * 16 + 4 * q, F - 4, bu[j]);
+    }
+    const int c = col[p] + (NS > 1 ? c8 : 4 * q);
+    const bool there = n0 + c < F;
+    const uint32_t at = (uint32_t)(row[p] + l15), oz = there ? at * zp + c * 2 : kOob, og = there ? at * gp + c * 2 : kOob;
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      uint32_t w[3][2][2];   // gate, up, g
+#pragma unroll
+      for (int j = 0; j < (NS > 1 ? 2 : 1); ++j) {
+        const f32x4_t a = NS > 1 ? acc[2 * p][i][j] : acc[0][i][0], u = NS > 1 ? acc[(2 * p + 1) % NS][i][j] : acc[0][i][1];
+        float f[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) f[r] = gate_f<GATE>(a[r] + bg[j][r]) * (u[r] + bu[j][r]);
+        w[0][j][0] = pack_bf16x2(a[0], a[1]); w[0][j][1] = pack_bf16x2(a[2], a[3]);
+        w[1][j][0] = pack_bf16x2(u[0], u[1]); w[1][j][1] = pack_bf16x2(u[2], u[3]);
+        w[2][j][0] = pack_bf16x2(f[0], f[1]); w[2][j][1] = pack_bf16x2(f[2], f[3]);
+      }
+      if constexpr (NS > 1) {
+        u32x4_t out[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          const u32x2_t x = __builtin_amdgcn_permlane16_swap(w[k][0][0], w[k][1][0], false, false);
+          const u32x2_t y = __builtin_amdgcn_permlane16_swap(w[k][0][1], w[k][1][1], false, false);
+          out[k] = u32x4_t{x[0], y[0], x[1], y[1]};
+        }
+        __builtin_amdgcn_raw_buffer_store_b128(out[0], rz, oz + i * 16 * zp, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(out[1], ru, oz + i * 16 * zp, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(out[2], rg, og + i * 16 * gp, 0, 0);
+      } else {
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{w[0][0][0], w[0][0][1]}, rz, oz + i * 16 * zp, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{w[1][0][0], w[1][0][1]}, ru, oz + i * 16 * zp, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{w[2][0][0], w[2][0][1]}, rg, og + i * 16 * gp, 0, 0);
+      }
+    }
+  }
+}
+// Backward: the product is dg; dz_gate = dg f'(a) c, dz_up = dg f(a), from z as the forward stored it, and (part) their column sums over blocks of RB * 16
+// rows.  The exchange that leaves a lane with eight consecutive columns is made in fp32: dg is not rounded.
+template <int GATE, int BM, int BN, int NS, int RB>
+__device__ __forceinline__ void gated_grad_store(const StripAcc<NS, RB>& acc, const int (&row)[NS], const int (&col)[NS], const GatedArgs& e, int M, int m0,
+                                                 int n0) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4, F = e.inner, c8 = 16 * (q & 1) + 8 * (q >> 1);
+  const uint32_t pitch = (uint32_t)F * 4, records = (uint32_t)(min(BM, M - m0) - 1) * pitch + min(BN, F - n0) * 2;
+  const size_t first = (size_t)m0 * 2 * F + n0;
+  const auto rza = __builtin_amdgcn_make_buffer_rsrc(e.z + first, 0, records, 0x00020000), rzu = __builtin_amdgcn_make_buffer_rsrc(e.z + first + F, 0, records, 0x00020000);
+  const auto rda = __builtin_amdgcn_make_buffer_rsrc(e.g + first, 0, records, 0x00020000), rdu = __builtin_amdgcn_make_buffer_rsrc(e.g + first + F, 0, records, 0x00020000);
+#pragma unroll
+  for (int b = 0; b < NS; ++b) {
+    const int c = col[b] + c8;
+    const uint32_t off = n0 + c < F ? (uint32_t)(row[b] + l15) * pitch + c * 2 : kOob;
+    constexpr int kAhead = NS * RB > 12 ? 2 : RB;   // blocks of rows requested together: as many as the registers allow
+    u32x4_t za[kAhead], zu[kAhead];
+    float ba[8], bu[8], sa[8], su[8];
+    load_bias<8>(e.bias, n0 + c, F - 8, ba);
+    load_bias<8>(e.bias ? e.bias + F : nullptr, n0 + c, F - 8, bu);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sa[j] = su[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      if (i % kAhead == 0) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          za[k] = __builtin_amdgcn_raw_buffer_load_b128(rza, off + (i + k) * 16 * pitch, 0, 0);
+          zu[k] = __builtin_amdgcn_raw_buffer_load_b128(rzu, off + (i + k) * 16 * pitch, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      float dg[8], a[8], u[8];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const u32x2_t x = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[b][i][0][r]), __float_as_uint(acc[b][i][1][r]), false, false);
+        dg[r] = __uint_as_float(x[0]);
+        dg[4 + r] = __uint_as_float(x[1]);
+      }
+      Vec16<bf16_t> v;
+      v.raw = __builtin_bit_cast(uint4, za[i % kAhead]);
+      v.unpack(a);
+      v.raw = __builtin_bit_cast(uint4, zu[i % kAhead]);
+      v.unpack(u);
+      const bool there = m0 + row[b] + i * 16 + l15 < M;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float d;
+        const float f = gate_grad_f<GATE>(a[j] + ba[j], &d);
+        a[j] = dg[j] * d * (u[j] + bu[j]);
+        u[j] = dg[j] * f;
+        sa[j] += there ? a[j] : 0.f;
+        su[j] += there ? u[j] : 0.f;
+      }
+      v.pack(a);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v.raw), rda, off + i * 16 * pitch, 0, 0);
+      v.pack(u);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v.raw), rdu, off + i * 16 * pitch, 0, 0);
+    }
+    if (e.part) {   // the sixteen rows of a block are lanes l15
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        sa[j] += row_rotate<8>(sa[j]); su[j] += row_rotate<8>(su[j]);
+        sa[j] += row_rotate<4>(sa[j]); su[j] += row_rotate<4>(su[j]);
+        sa[j] += row_rotate<2>(sa[j]); su[j] += row_rotate<2>(su[j]);
+        sa[j] += row_rotate<1>(sa[j]); su[j] += row_rotate<1>(su[j]);
+      }
+      if (l15 == 0 && n0 + c < F && m0 + row[b] < M) {
+        float* p = e.part + (size_t)((m0 + row[b]) / (RB * 16)) * 2 * F + n0 + c;
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+          *reinterpret_cast<float4*>(p + h) = make_float4(sa[h], sa[h + 1], sa[h + 2], sa[h + 3]);
+          *reinterpret_cast<float4*>(p + F + h) = make_float4(su[h], su[h + 1], su[h + 2], su[h + 3]);
+        }
+      }
+    }
+  }
+}
+
 // One 256 x 256 tile over k-tiles kt0 .. kt1-1, written either in the caller's output form (slab == nullptr) or
 // as a dense 256 x 256 fp32 slab.
 template <bool TA, bool TB, int OUT>
@@ -983,8 +1141,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, void* Cv, float* sl
 //   computes   A0 x B0, A0 x B1   A1 x B1, A1 x B0
 // What a phase has read may be refilled from the next phase's memory part on; a request has three phases to land, and the wait at the end of
 // a memory part leaves the eight loads in flight that are younger than what the next one reads.
-template <bool TB>
-__device__ __forceinline__ void gemm_mid_mainloop(f32x4_t (&acc)[4][2][3], const GemmArgs& g, int m0, int n0, char* smem) {
+template <bool TB, bool GAP = false>
+__device__ __forceinline__ void gemm_mid_mainloop(f32x4_t (&acc)[4][2][3], const GemmArgs& g, int m0, int n0, char* smem, int gap = 128) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const bf16_t* a_base = g.A + (size_t)m0 * g.lda;
   const bf16_t* b_base = TB ? g.B + n0 : g.B + (size_t)n0 * g.ldb;
@@ -996,7 +1154,7 @@ __device__ __forceinline__ void gemm_mid_mainloop(f32x4_t (&acc)[4][2][3], const
   HalfLoad<false> la;
   HalfLoad<TB, 96> lb;
   la.init(g.lda, g.M - m0, wave, lane);
-  lb.init(g.ldb, g.N - n0, wave, lane);
+  lb.template init<GAP>(g.ldb, g.N - n0, wave, lane, gap);
   FragRead<false, 2> fa;
   FragRead<TB, 3> fb;
   fa.init(smem, (wave >> 1) * 32, lane);
@@ -1096,8 +1254,10 @@ __device__ __forceinline__ void gemm_mid_mainloop(f32x4_t (&acc)[4][2][3], const
 }
 
 constexpr int kMidN = 192;
-template <bool TB>
-__device__ __forceinline__ void gemm_mid_tile(const GemmArgs& g, void* Cv, int m0, int n0, char* smem) {
+// EPI_GATED: half 0 is the gate's 96 columns, half 1 the up projection's (g.N, n0: inner columns), so that acc[2 ha] and acc[2 ha + 1] belong together
+template <bool TB, class EPI = Epi<EPI_PLAIN>, class E = GeluArgs<bf16_t>>
+__device__ __forceinline__ void gemm_mid_tile(const GemmArgs& g, void* Cv, int m0, int n0, char* smem, const E& e = {}) {
+  constexpr bool kGated = EPI::kKind == EPI_GATED;
   f32x4_t acc[4][2][3];
 #pragma unroll
   for (int q = 0; q < 4; ++q)
@@ -1105,8 +1265,28 @@ __device__ __forceinline__ void gemm_mid_tile(const GemmArgs& g, void* Cv, int m
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 3; ++j) acc[q][i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  gemm_mid_mainloop<TB>(acc, g, m0, n0, smem);
+  gemm_mid_mainloop<TB, kGated>(acc, g, m0, n0, smem, kGated ? g.N : 128);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = (wave >> 1) * 32, wn = (wave & 1) * 96;
+  if constexpr (kGated) {   // of a wave's 48 columns two blocks of 16 as a strip, the third by itself
+    StripAcc<4, 2> two;
+    StripAcc<1, 2> one[2];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        two[q][i][0] = acc[q][i][0];
+        two[q][i][1] = acc[q][i][1];
+        one[q >> 1][0][i][q & 1] = acc[q][i][2];
+      }
+    const int row[2] = {wm, wm + 128}, col[2] = {wn / 2, wn / 2}, third = wn / 2 + 32;
+    with_gate(e.gate, [&](auto gate) {
+      constexpr int G = decltype(gate)::value;
+      gated_store<G, kBM, kMidN / 2, 4, 2>(two, row, col, e, g.M, m0, n0);
+      gated_store<G, kBM, kMidN / 2, 1, 2>(one[0], row, &third, e, g.M, m0, n0);
+      gated_store<G, kBM, kMidN / 2, 1, 2>(one[1], row + 1, &third, e, g.M, m0, n0);
+    });
+    return;
+  }
   StripAcc<6, 2> out;   // strip 3 * ha + p: rows ha * 128 + wm .., columns wn + 32 p ..
   int row[6], col[6];
 #pragma unroll
@@ -1120,6 +1300,10 @@ __device__ __forceinline__ void gemm_mid_tile(const GemmArgs& g, void* Cv, int m
 #pragma unroll
         for (int j = 0; j < 2; ++j) out[3 * ha + p][i][j] = acc[2 * ha + (2 * p + j) / 3][i][(2 * p + j) % 3];
     }
+  if constexpr (EPI::kKind == EPI_GATED_GRAD) {
+    with_gate(e.gate, [&](auto gate) { gated_grad_store<decltype(gate)::value, kBM, kMidN, 6, 2>(out, row, col, e, g.M, m0, n0); });
+    return;
+  }
   ColumnAdd<6, Epi<EPI_PLAIN>> add;
   add.load(g.bias, col, g.N, n0);
   gemm_epilogue<OUT_BF16, kBM, kMidN, 6, 2>(out, row, col, Cv, g.ldc, add, g.M, g.N, m0, n0);
@@ -1218,6 +1402,18 @@ template <bool KSLOW, int ROWS> struct SmallLoad {
     kstep = KSLOW ? (uint32_t)(BK * ld * 2) : (uint32_t)(BK * 2);
     plain = ld >= 128;
   }
+  // k-slow: U rows of the block and U rows `gap` further on in turn; rows_left counts either's
+  template <int U> __device__ __forceinline__ void init_pairs(size_t ld, int rows_left, int gap, int wave, int lane) {
+    static_assert(KSLOW && U % 8 == 0);
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const int k = kpos(i, wave, lane), c = ((lane & (ROWS / 8 - 1)) ^ kslow_swizzle<ROWS>(k)) * 8;
+      const int row = c / (2 * U) * U + c % U;
+      off[i] = row < rows_left ? (uint32_t)(((size_t)k * ld + row + (c / U % 2 ? gap : 0)) * 2) - i * 1024u : kOob;
+    }
+    kstep = (uint32_t)(BK * ld * 2);
+    plain = ld >= 128;
+  }
   // LEAN: the caller knows that the k-tile lies inside K whole and that plain is set
   template <bool LEAN = false> __device__ __forceinline__ void issue(rsrc_t r, char* tile, int wave, int lane, int kt, int kend) const {
     char* dst = tile + wave * L * 1024;
@@ -1276,8 +1472,11 @@ template <int BM, int BN, int S, int KG> struct SmallGeom {
   static constexpr int kThreads = KG * kSmallThreads;
 };
 
-template <bool TA, bool TB, int OUT, int BM, int BN, int S, int KG, class EPI>
-__device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, void* Cv, int m0, int n0, char* smem, const GeluArgs<bf16_t>& e) {
+// EPI_GATED: g.N and n0 count inner columns; a tile is BN / 2 of the gate's and BN / 2 of the up projection's columns, 32 (a wave of one strip: 16) of
+// either in turn.
+template <bool TA, bool TB, int OUT, int BM, int BN, int S, int KG, class EPI, class E>
+__device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, void* Cv, int m0, int n0, char* smem, const E& e) {
+  constexpr bool kGated = EPI::kKind == EPI_GATED || EPI::kKind == EPI_GATED_GRAD;
   typedef SmallGeom<BM, BN, S, KG> G;
   constexpr int NS = BN / 64, RB = BM / 32, kLoads = (BM + BN) / 32;   // strips, row blocks; loads per wave and k-tile
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
@@ -1294,7 +1493,8 @@ __device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, void* Cv, int
   SmallLoad<TA, BM> la;
   SmallLoad<TB, BN> lb;
   la.init(g.lda, g.M - m0, wave, lane);
-  lb.init(g.ldb, g.N - n0, wave, lane);
+  if constexpr (EPI::kKind == EPI_GATED) lb.template init_pairs<(BN > 64 ? 32 : 16)>(g.ldb, g.N - n0, g.N, wave, lane);
+  else lb.init(g.ldb, g.N - n0, wave, lane);
   SmallRead<TA, BM> fa;
   SmallRead<TB, BN> fb;
   fa.init(ring, wm, lane);
@@ -1315,9 +1515,13 @@ __device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, void* Cv, int
   GeluRows<NS, RB> z;
   constexpr bool kReadsZ = EPI::kKind == EPI_GELU_GRAD || EPI::kKind == EPI_BDA;
   constexpr bool kAddAhead = OUT == OUT_BF16 && (!kReadsZ || NS == 1);   // (128 x 128 tiles with z: registers would spill; += : a bias is rare)
-  auto load_add = [&] { add.load(EPI::kKind == EPI_PLAIN ? g.bias : e.b, col, g.N, n0); };
+  auto load_add = [&] {
+    if constexpr (!kGated) add.load(EPI::kKind == EPI_PLAIN ? g.bias : e.b, col, g.N, n0);
+  };
   if (kAddAhead) load_add();
-  if (kReadsZ && kg == 0) z.template load<BM, BN>(e.z, row, col, g.ldc, g.M, g.N, m0, n0);
+  if constexpr (kReadsZ) {
+    if (kg == 0) z.template load<BM, BN>(e.z, row, col, g.ldc, g.M, g.N, m0, n0);
+  }
 #pragma unroll
   for (int i = 0; i < S; ++i) request(i, i);
   StripAcc<NS, RB> acc;
@@ -1392,7 +1596,14 @@ __device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, void* Cv, int
       for (int i = 0; i < RB * 2; ++i) acc[b][i >> 1][i & 1] += sum[(b * RB * 2 + i) * 64];
   }
   if (!kAddAhead) load_add();
-  gemm_epilogue<OUT, BM, BN, NS, RB, EPI>(acc, row, col, Cv, g.ldc, add, g.M, g.N, m0, n0, e, z);
+  if constexpr (EPI::kKind == EPI_GATED) {
+    const int inner = wn / 2;   // of the wave's one pair
+    with_gate(e.gate, [&](auto gate) { gated_store<decltype(gate)::value, BM, BN / 2, NS, RB>(acc, row, &inner, e, g.M, m0, n0); });
+  } else if constexpr (EPI::kKind == EPI_GATED_GRAD) {
+    with_gate(e.gate, [&](auto gate) { gated_grad_store<decltype(gate)::value, BM, BN, NS, RB>(acc, row, col, e, g.M, m0, n0); });
+  } else {
+    gemm_epilogue<OUT, BM, BN, NS, RB, EPI>(acc, row, col, Cv, g.ldc, add, g.M, g.N, m0, n0, e, z);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1418,8 +1629,10 @@ __device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, void* Cv, int
 // ------------------------------------------------------------------------------------------------
 constexpr int kWideM = 256, kWideN = 128, kWideLag = 3;
 constexpr int kWideStage = (kWideM + kWideN) * BK * 2, kWideSmem = 3 * kWideStage;
-template <bool TB>
-__device__ __forceinline__ void gemm_wide_tile(const GemmArgs& g, void* Cv, int m0, int n0, char* smem) {
+// EPI_GATED: half 0 is the gate's 64 columns, half 1 the up projection's (g.N, n0: inner columns)
+template <bool TB, class EPI = Epi<EPI_PLAIN>, class E = GeluArgs<bf16_t>>
+__device__ __forceinline__ void gemm_wide_tile(const GemmArgs& g, void* Cv, int m0, int n0, char* smem, const E& e = {}) {
+  constexpr bool kGated = EPI::kKind == EPI_GATED;
   const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave8 & 3, grp = wave8 >> 2;
   const bf16_t* a_base = g.A + (size_t)m0 * g.lda;
   const bf16_t* b_base = TB ? g.B + n0 : g.B + (size_t)n0 * g.ldb;
@@ -1434,7 +1647,7 @@ __device__ __forceinline__ void gemm_wide_tile(const GemmArgs& g, void* Cv, int 
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     la[h].init(g.lda, g.M - m0, wave, lane, h * 128);
-    lb[h].init(g.ldb, g.N - n0, wave, lane, h * 64);
+    lb[h].init(g.ldb, g.N - n0 + (kGated ? h * g.N : 0), wave, lane, h * (kGated ? g.N : 64));
   }
   SmallRead<false, 128> fa;
   SmallRead<TB, 64> fb;
@@ -1581,6 +1794,14 @@ __device__ __forceinline__ void gemm_wide_tile(const GemmArgs& g, void* Cv, int 
     }
   const int rm = grp * 128 + (wave >> 1) * 64, cn = (wave & 1) * 32;
   const int row[2] = {rm, rm}, col[2] = {cn, cn + 64};
+  if constexpr (kGated) {
+    with_gate(e.gate, [&](auto gate) { gated_store<decltype(gate)::value, kWideM, kWideN / 2, 2, 4>(mine, row, col, e, g.M, m0, n0); });
+    return;
+  }
+  if constexpr (EPI::kKind == EPI_GATED_GRAD) {
+    with_gate(e.gate, [&](auto gate) { gated_grad_store<decltype(gate)::value, kWideM, kWideN, 2, 4>(mine, row, col, e, g.M, m0, n0); });
+    return;
+  }
   ColumnAdd<2, Epi<EPI_PLAIN>> add;
   add.load(g.bias, col, g.N, n0);
   gemm_epilogue<OUT_BF16, kWideM, kWideN, 2, 4>(mine, row, col, Cv, g.ldc, add, g.M, g.N, m0, n0);
@@ -2454,6 +2675,156 @@ int launch_gemm_gelu_bwd(int dtype, int gelu_mode, const void* dg, const void* w
     if (rc != PTDP_OK || (rc = L.status()) != PTDP_OK) return rc;
   }
   return colsum_finish((const float*)scratch, (M + rows - 1) / rows, N, dbias, nullptr, N, st, defer);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Gated feed-forward block: z[M, 2 F] = u[M, K] w[K, 2 F] and g = f(z_gate + b) (z_up + b) in one kernel, and dg = dy w2^T with what makes dz of it.
+// The forward's tile is the plain kernels' with half of its columns from the gate's and half from the up projection's half of w, so that
+// the same lane ends up with both and nothing is read back; what bounds it is what bounds the product.
+// ------------------------------------------------------------------------------------------------
+template <bool TB>
+__global__ void __launch_bounds__(kGemmThreads)
+gated_large_kernel(GemmArgs g, GatedArgs e) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  // tiles as in gemm_dp_tile; forward (TB): 128 inner columns each, g.N counts those
+  constexpr int kCols = TB ? 128 : kBN;
+  const int tiles_m = (g.M + kBM - 1) / kBM, tiles_n = (g.N + kCols - 1) / kCols, xcd = blockIdx.x & 7, nx = tiles_n / 8, own = tiles_m * nx;
+  int t = blockIdx.x >> 3, cols = nx, first = xcd, step = 8;
+  if (t >= own) {
+    cols = tiles_n - 8 * nx;
+    first = 8 * nx;
+    step = 1;
+    const int rest = cols * tiles_m, per_xcd = (rest + 7) / 8;
+    t -= own;
+    if (t >= per_xcd) return;
+    t += xcd * per_xcd;
+    if (t >= rest) return;
+  }
+  const int per_group = 8 * cols, grp = t / per_group, in_grp = t % per_group, gm = min(8, tiles_m - grp * 8);
+  const int m0 = (grp * 8 + in_grp % gm) * kBM, n0 = ((in_grp / gm) * step + first) * kCols;
+  TileAcc acc;
+  zero_acc<4, 4>(acc);
+  gemm_mainloop<false, TB, TB>(acc, g, m0, n0, 0, (g.K + BK - 1) / BK, smem, TB ? g.N : 128);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = (wave >> 2) * 64, wn = (wave & 3) * 32;
+  if constexpr (TB) {
+    const int row[2] = {wm, wm + 128}, col[2] = {wn, wn};
+    with_gate(e.gate, [&](auto gate) { gated_store<decltype(gate)::value, kBM, 128, 4, 4>(acc, row, col, e, g.M, m0, n0); });
+  } else {
+    const int row[4] = {wm, wm, wm + 128, wm + 128}, col[4] = {wn, wn + 128, wn, wn + 128};
+    with_gate(e.gate, [&](auto gate) { gated_grad_store<decltype(gate)::value, kBM, kBN, 4, 4>(acc, row, col, e, g.M, m0, n0); });
+  }
+}
+template <bool TB> static int launch_gated_large(const GemmArgs& g, const GatedArgs& e, hipStream_t st) {
+  const auto kern = gated_large_kernel<TB>;
+  static once_flag_t done[kMaxDevices];
+  if (set_dynamic_smem(reinterpret_cast<const void*>(kern), kGemmSmem, done) != PTDP_OK) return PTDP_E_HIP;
+  const int blocks = 8 * (int)busiest_xcd((g.M + kBM - 1) / kBM, TB ? (g.N + 127) / 128 : (g.N + kBN - 1) / kBN);
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(kGemmThreads), kGemmSmem, st, g, e);
+  return PTDP_OK;
+}
+// TB: forward (NN), otherwise backward (NT); tiles numbered as in gemm_small_id
+template <bool TB, int BM, int BN, int S, int KG>
+__global__ void __launch_bounds__(KG * kSmallThreads, 2)
+gated_small_kernel(GemmArgs g, GatedArgs e) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr int kCols = TB ? BN / 2 : BN;
+  const int tiles_m = (g.M + BM - 1) / BM, tiles_n = (g.N + kCols - 1) / kCols, tiles = tiles_m * tiles_n;
+  const int id = blockIdx.x, per_xcd = (tiles + 7) / 8, t = (id & 7) * per_xcd + (id >> 3);
+  if ((id >> 3) >= per_xcd || t >= tiles) return;
+  const int grp = t / (8 * tiles_n), in_grp = t - grp * 8 * tiles_n, gm = min(8, tiles_m - grp * 8);
+  gemm_small_tile<false, TB, OUT_BF16, BM, BN, S, KG, Epi<TB ? EPI_GATED : EPI_GATED_GRAD>>(g, nullptr, (grp * 8 + in_grp % gm) * BM, (in_grp / gm) * kCols,
+                                                                                         smem, e);
+}
+// 256 x 128 and (MID) 256 x 192 tiles
+template <bool TB, bool MID>
+__global__ void __launch_bounds__(kGemmThreads)
+gated_medium_kernel(GemmArgs g, GatedArgs e) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr int kCols = (MID ? kMidN : kWideN) / (TB ? 2 : 1);
+  const int tiles_m = (g.M + kBM - 1) / kBM, tiles_n = (g.N + kCols - 1) / kCols, tiles = tiles_m * tiles_n;
+  const int id = blockIdx.x, per_xcd = (tiles + 7) / 8, t = (id & 7) * per_xcd + (id >> 3);
+  if ((id >> 3) >= per_xcd || t >= tiles) return;
+  const int grp = t / (8 * tiles_n), in_grp = t - grp * 8 * tiles_n, gm = min(8, tiles_m - grp * 8);
+  const int m0 = (grp * 8 + in_grp % gm) * kBM, n0 = (in_grp / gm) * kCols;
+  using EPI = Epi<TB ? EPI_GATED : EPI_GATED_GRAD>;
+  if constexpr (MID) gemm_mid_tile<TB, EPI>(g, nullptr, m0, n0, smem, e);
+  else gemm_wide_tile<TB, EPI>(g, nullptr, m0, n0, smem, e);
+}
+template <bool TB, bool MID> static int launch_gated_medium(const GemmArgs& g, const GatedArgs& e, hipStream_t st) {
+  const auto kern = gated_medium_kernel<TB, MID>;
+  static once_flag_t done[kMaxDevices];
+  constexpr int smem = MID ? kGemmSmem : kWideSmem;
+  if (set_dynamic_smem(reinterpret_cast<const void*>(kern), smem, done) != PTDP_OK) return PTDP_E_HIP;
+  hipLaunchKernelGGL(kern, dim3(small_blocks<kBM, (MID ? kMidN : kWideN) / (TB ? 2 : 1)>(g.M, g.N)), dim3(kGemmThreads), smem, st, g, e);
+  return PTDP_OK;
+}
+template <bool TB, int BM, int BN, int S, int KG>
+static int launch_gated_small(const GemmArgs& g, const GatedArgs& e, hipStream_t st) {
+  const auto kern = gated_small_kernel<TB, BM, BN, S, KG>;
+  static once_flag_t done[kMaxDevices];
+  constexpr int smem = SmallGeom<BM, BN, S, KG>::kSmem;
+  if (set_dynamic_smem(reinterpret_cast<const void*>(kern), smem, done) != PTDP_OK) return PTDP_E_HIP;
+  hipLaunchKernelGGL(kern, dim3(small_blocks<BM, TB ? BN / 2 : BN>(g.M, g.N)), dim3(KG * kSmallThreads), smem, st, g, e);
+  return PTDP_OK;
+}
+template <bool TB> static int launch_gated_form(int form, const GemmArgs& g, const GatedArgs& e, hipStream_t st) {
+  switch (form) {
+    case 0: return launch_gated_small<TB, 128, 128, 2, 1>(g, e, st);
+    case 1: return launch_gated_small<TB, 128, 128, 2, 2>(g, e, st);
+    case 2: return launch_gated_small<TB, 128, 64, 3, 2>(g, e, st);
+    case 3: return launch_gated_small<TB, 64, 64, 4, 2>(g, e, st);
+    case 4: return launch_gated_small<TB, 128, 64, 2, 1>(g, e, st);
+    case 5: return launch_gated_medium<TB, false>(g, e, st);
+    case kMidForm: return launch_gated_medium<TB, true>(g, e, st);
+    default: return launch_gated_large<TB>(g, e, st);
+  }
+}
+// The form of a product of N columns, -1: 256 x 256 tiles: the plain product's choice.
+static int gated_form(int mode, int M, int N, int K) {
+  SplitPlan P;
+  return choose_form(mode, M, N, K, 0, 0, 0, 0, &P);
+}
+// what the kernels address: operands below 2 GiB, rows of z below kWideRow
+bool gated_mlp_fits(int dtype, int rows, int width, int inner) {
+  const uint64_t esz = dtype == PTDP_BF16 ? 2 : 4, most = 0x7fffffffull;
+  return (uint64_t)rows * width * esz < most && (uint64_t)width * 2 * inner * esz < most && (uint64_t)inner * 2 * esz < kWideRow &&
+         (uint64_t)rows * inner * esz < (most << 4);
+}
+int launch_gated_mlp_fwd(int dtype, int gate, const void* u, const void* w, const void* bias, void* z, void* g, int rows, int width, int inner,
+                         hipStream_t st) {
+  if (dtype == PTDP_F32) {
+    const int rc = launch_gemm(dtype, PTDP_GEMM_NN, u, w, z, nullptr, rows, 2 * inner, width, 0, 0, nullptr, 0, st);
+    return rc != PTDP_OK ? rc : launch_gated_act(gate, (const float*)z, (const float*)bias, (float*)g, rows, inner, st);
+  }
+  Launch L(PTDP_K_GEMM_NN, 4.0 * rows * inner * width, st);
+  GemmArgs a = bf16_args<false, true>(u, w, nullptr, rows, 2 * inner, width);
+  a.N = inner;   // (ldb stays the whole row)
+  const GatedArgs e{(const bf16_t*)bias, (bf16_t*)z, (bf16_t*)g, nullptr, inner, gate};
+  const int rc = launch_gated_form<true>(gated_form(PTDP_GEMM_NN, rows, 2 * inner, width), a, e, st);
+  return rc != PTDP_OK ? rc : L.status();
+}
+// workspace: the column sums' partial sums; fp32: and dg
+static size_t gated_part_bytes(int rows, int inner) { return (colsum_scratch_bytes(rows, 2 * inner) + 255) & ~(size_t)255; }
+size_t gated_mlp_workspace_bytes(int dtype, int rows, int width, int inner) {
+  return gated_part_bytes(rows, inner) + (dtype == PTDP_F32 ? (size_t)rows * inner * sizeof(float) : 0);
+}
+int launch_gated_mlp_bwd(int dtype, int gate, const void* dy, const void* w2, const void* z, const void* bias, void* dz, float* dbias, void* workspace,
+                         int rows, int width, int inner, hipStream_t st) {
+  float* part = (float*)workspace;
+  int parts, rc;
+  if (dtype == PTDP_BF16) {
+    const int form = gated_form(PTDP_GEMM_NT, rows, inner, width), per = form < 0 || form == 5 ? 64 : form == kMidForm ? 32 : kSmallCost[0][form].bm / 2;   // rows of a partial sum
+    parts = (rows + per - 1) / per;
+    Launch L(PTDP_K_GEMM_NT, 2.0 * rows * inner * width, st);
+    const GemmArgs a = bf16_args<false, false>(dy, w2, nullptr, rows, inner, width);
+    const GatedArgs e{(const bf16_t*)bias, (bf16_t*)const_cast<void*>(z), (bf16_t*)dz, dbias ? part : nullptr, inner, gate};
+    if ((rc = launch_gated_form<false>(form, a, e, st)) != PTDP_OK || (rc = L.status()) != PTDP_OK) return rc;
+  } else {
+    float* dg = (float*)((char*)workspace + gated_part_bytes(rows, inner));
+    if ((rc = launch_gemm(dtype, PTDP_GEMM_NT, dy, w2, dg, nullptr, rows, inner, width, 0, 0, nullptr, 0, st)) != PTDP_OK) return rc;
+    if ((rc = launch_gated_act_bwd(gate, dg, (const float*)z, (const float*)bias, (float*)dz, dbias ? part : nullptr, rows, inner, &parts, st)) != PTDP_OK) return rc;
+  }
+  return dbias ? colsum_finish(part, parts, 2 * inner, dbias, nullptr, 2 * inner, st) : PTDP_OK;
 }
 
 }  // namespace ptdp

@@ -1,10 +1,10 @@
-"""Pins of the oracles of rotary positions and attention under spans: differences, closed forms, and independent derivations."""
+"""Pins of the oracles of rotary positions, attention under spans and the gated feed-forward block: differences, closed forms, and independent derivations."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import gpt_layer as L
-from oracle import rotary, span_attention as A
+from oracle import gated_mlp as G, rotary, span_attention as A
 
 
 @pytest.mark.parametrize("neighbours", [False, True])
@@ -114,3 +114,18 @@ def test_hidden_elements_are_not_touched():
     with np.errstate(invalid="ignore"):
         got = A.forward(bad, lo, hi, heads, heads, 0.3)[0], A.backward(bad_d, bad, lo, hi, heads, heads, 0.3)
     assert np.array_equal(got[0][:5], want[0][:5]) and np.array_equal(got[1][:5], want[1][:5])
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu_erf", "gelu_tanh", "sigmoid", "relu"])
+def test_gated_block_by_differences_and_against_torch(kind):
+    rng = np.random.default_rng(6)
+    u, w, w2, b, dy = (rng.normal(size=n) for n in ((7, 5), (5, 12), (6, 5), (12,), (7, 5)))
+    z, g = G.forward(kind, u, w, b)
+    F = torch.nn.functional
+    f = dict(silu=F.silu, gelu_erf=F.gelu, gelu_tanh=lambda a: F.gelu(a, approximate="tanh"), sigmoid=torch.sigmoid, relu=F.relu)[kind]
+    t = torch.tensor(u) @ torch.tensor(w) + torch.tensor(b)
+    assert np.allclose(g, (f(t[:, :6]) * t[:, 6:]).numpy())
+    dz = G.backward(kind, dy, w2, z, b)
+    d = rng.normal(size=z.shape)
+    loss = lambda x: ((G.act(kind, x[:, :6] + b[:6])[0] * (x[:, 6:] + b[6:])) @ w2 * dy).sum()  # noqa: E731
+    assert np.isclose((loss(z + 1e-6 * d) - loss(z - 1e-6 * d)) / 2e-6, (dz * d).sum(), rtol=1e-6)
