@@ -527,6 +527,9 @@ int ptdp_gated_mlp_fwd(int dtype, int gate, const void* u, const void* w, const 
 int ptdp_gated_mlp_bwd(int dtype, int gate, const void* dy, const void* w2, const void* z, const void* bias, void* dz, float* dbias, void* workspace,
                        int rows, int width, int inner, void* stream);
 size_t ptdp_gated_mlp_workspace_bytes(int dtype, int rows, int width, int inner);
+/* Host only: the tiles of such a bf16 call (back = 0: ptdp_gated_mlp_fwd), as ptdp_gemm_form tells them of a product; a forward tile's columns are
+ * half the gate's and half the up projection's.  Returns 0, PTDP_E_INVALID_ARG, PTDP_E_UNSUPPORTED or PTDP_E_NULL_PTR. */
+int ptdp_gated_mlp_form(int back, int rows, int width, int inner, int* tile_m, int* tile_n, int* wave_groups);
 
 /* ---------------------------------------------------------------- ceilings */
 /* What the chip is seen to do, for reading roofline fractions: a loop of

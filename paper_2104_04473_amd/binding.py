@@ -150,6 +150,7 @@ SIGNATURES = {
     "ptdp_gated_mlp_fwd": (_i, [_i, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp]),
     "ptdp_gated_mlp_bwd": (_i, [_i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp]),
     "ptdp_gated_mlp_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "ptdp_gated_mlp_form": (_i, [_i, _i, _i, _i, C.POINTER(_i), C.POINTER(_i), C.POINTER(_i)]),
     "ptdp_ceiling_mfma": (_i, [_vp, _i, _i, _i, C.POINTER(C.c_double), _vp]),
     "ptdp_ceiling_copy": (_i, [_vp, _vp, _sz, _vp]),
     "ptdp_prof_enable": (_i, [_i]),

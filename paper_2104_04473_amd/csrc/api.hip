@@ -1055,6 +1055,13 @@ static int check_gated(int dtype, int gate, int rows, int width, int inner) {
 size_t ptdp_gated_mlp_workspace_bytes(int dtype, int rows, int width, int inner) {
   return check_gated(dtype, PTDP_GATE_SILU, rows, width, inner) == PTDP_OK ? gated_mlp_workspace_bytes(dtype, rows, width, inner) : 0;
 }
+int ptdp_gated_mlp_form(int back, int rows, int width, int inner, int* tile_m, int* tile_n, int* wave_groups) {
+  PTDP_TRY(check_gated(PTDP_BF16, PTDP_GATE_SILU, rows, width, inner));
+  if ((back != 0 && back != 1) || rows == 0) return PTDP_E_INVALID_ARG;
+  if (!tile_m || !tile_n || !wave_groups) return PTDP_E_NULL_PTR;
+  gated_mlp_form_query(back, rows, width, inner, tile_m, tile_n, wave_groups);
+  return PTDP_OK;
+}
 int ptdp_gated_mlp_fwd(int dtype, int gate, const void* u, const void* w, const void* bias, void* z, void* g, int rows, int width, int inner,
                        void* stream) {
   PTDP_TRY(check_gated(dtype, gate, rows, width, inner));

@@ -273,6 +273,7 @@ int launch_gated_mlp_fwd(int dtype, int gate, const void* u, const void* w, cons
                          hipStream_t st);
 size_t gated_mlp_workspace_bytes(int dtype, int rows, int width, int inner);
 int launch_gated_mlp_bwd(int dtype, int gate, const void* dy, const void* w2, const void* z, const void* bias, void* dz, float* dbias, void* workspace,
+void gated_mlp_form_query(int back, int rows, int width, int inner, int* tile_m, int* tile_n, int* groups);
                          int rows, int width, int inner, hipStream_t st);
 
 }  // namespace ptdp

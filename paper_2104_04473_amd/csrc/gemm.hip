@@ -2267,24 +2267,26 @@ constexpr int kWideSteps = 120;
 // up to 1.6 times the above (128 x 64, 16 workgroups, 100 k-tiles).
 constexpr int kManyRounds = 16, kManySteps = 32;
 
+// of form f, infinite where it is not considered; min_steps: k-tiles from which two wave groups are
+static double small_time(int rmw, int f, int n, const int* M, const int* N, int K, int min_steps) {
+  const int ncu = compute_units(), nk = (K + BK - 1) / BK;
+  const SmallCost& c = kSmallCost[rmw][f];
+  if ((c.groups > 1 && nk < min_steps) || (c.bm == kWideM && nk > kWideSteps)) return INFINITY;
+  long long tiles = 0;
+  double mb = 0.0;
+  for (int j = 0; j < n; ++j) {
+    tiles += (long long)((M[j] + c.bm - 1) / c.bm) * ((N[j] + c.bn - 1) / c.bn);
+    mb += 2e-6 * ((double)M[j] + N[j]) * K;
+  }
+  if (tiles > (1 << 30) || (tiles > (long long)(kManyRounds - 1) * ncu && nk >= kManySteps)) return INFINITY;
+  const double w = (double)((tiles + ncu - 1) / ncu), steps = (nk + c.groups - 1) / c.groups;
+  return c.fixed + c.each * w + c.per_mb * mb + steps * (c.per_cu == 2 ? c.pair * (double)(int)(w / 2) + c.single * (w - 2 * (int)(w / 2)) : c.single * w);
+}
 // *time: of the best large form, then of the best of all
 static int small_form(int rmw, int n, const int* M, const int* N, int K, double* time) {
-  const int ncu = compute_units(), nk = (K + BK - 1) / BK;
   int best = -1;
   for (int f = 0; f < (rmw ? kSmallForms - 1 : kSmallForms); ++f) {
-    const SmallCost& c = kSmallCost[rmw][f];
-    if (c.groups > 1 && nk < kMinStepsForGroups) continue;
-    if (c.bm == kWideM && nk > kWideSteps) continue;
-    long long tiles = 0;
-    double mb = 0.0;
-    for (int j = 0; j < n; ++j) {
-      tiles += (long long)((M[j] + c.bm - 1) / c.bm) * ((N[j] + c.bn - 1) / c.bn);
-      mb += 2e-6 * ((double)M[j] + N[j]) * K;
-    }
-    if (tiles > (1 << 30)) continue;
-    if (tiles > (long long)(kManyRounds - 1) * ncu && nk >= kManySteps) continue;
-    const double w = (double)((tiles + ncu - 1) / ncu), steps = (nk + c.groups - 1) / c.groups;
-    const double t = c.fixed + c.each * w + c.per_mb * mb + steps * (c.per_cu == 2 ? c.pair * (double)(int)(w / 2) + c.single * (w - 2 * (int)(w / 2)) : c.single * w);
+    const double t = small_time(rmw, f, n, M, N, K, kMinStepsForGroups);
     if (t < *time) {
       *time = t;
       best = f;
@@ -2779,10 +2781,42 @@ template <bool TB> static int launch_gated_form(int form, const GemmArgs& g, con
     default: return launch_gated_large<TB>(g, e, st);
   }
 }
-// The form of a product of N columns, -1: 256 x 256 tiles: the plain product's choice.
+// The form of a product of N columns, -1: 256 x 256 tiles: the plain product's models, and for the backward's output stage what a call and
+// a compute unit's share of the outputs, in tiles, cost more (large tiles have least to run beside it).  64 x 64 tiles from five k-tiles on.
+// Over 430 random calls of 16 to 8192 rows, 264 to 12288 and 264 to 8192 columns the form taken is 1.1 % behind the best one on average forward
+// (1.37 times at worst), 0.4 % backward (1.19); with the plain product's models alone backward 1.5 % (1.40).  us, backward, 128 x 64 and 128 x 128
+// tiles: 5968 x 504 x 3768 71, 77; 256 x 128 and 256 x 256: 2048 x 4096 x 2816 50, 78; 256 x 192 and 256 x 256: 2919 x 1248 x 3384 45, 41.
+struct GatedCost { double call, tiles; };
+static const GatedCost kGatedGradCost[kSmallForms + 1] = {{1.0, 6.3}, {2.0, 6.0}, {0.5, 3.0}, {0.5, 1.0}, {0.0, 2.5}, {-2.0, 14.0}, {-0.5, 23.0}}, kGatedGradLarge = {4.0, 22.0};
+constexpr int kGatedMinSteps = 5;
 static int gated_form(int mode, int M, int N, int K) {
-  SplitPlan P;
-  return choose_form(mode, M, N, K, 0, 0, 0, 0, &P);
+  const bool back = mode == PTDP_GEMM_NT;
+  auto more = [&](const GatedCost& c, int bm, int bn) { return back ? c.call + c.tiles * M * N / ((double)bm * bn * compute_units()) : 0.0; };
+  double best_time, t;
+  const bool tall = 2 * M > kBM;   // tiles of 256 rows would be half empty: their models know little of that
+  large_plan(M, N, K, 0, 0, 0, 0, &best_time);
+  best_time = tall ? best_time + more(kGatedGradLarge, kBM, kBN) : INFINITY;
+  int best = -1;
+  for (int f = 0; f < kSmallForms; ++f) {
+    const SmallCost& c = kSmallCost[0][f];
+    if (c.bm == kBM && !tall) continue;
+    t = small_time(0, f, 1, &M, &N, K, c.bm == 64 ? kGatedMinSteps : kMinStepsForGroups) + more(kGatedGradCost[f], c.bm, c.bn);
+    if (t < best_time) {
+      best_time = t;
+      best = f;
+    }
+  }
+  const int rows = (M + kBM - 1) / kBM * kBM;   // as in choose_form
+  if (K > kMidShort && rows > kBM && 4 * (long long)M >= 3ll * rows && (mid_time(mode, M, N, K) + more(kGatedGradCost[kMidForm], kBM, kMidN)) * kMidMargin < best_time)
+    return kMidForm;
+  return best;
+}
+void gated_mlp_form_query(int back, int rows, int width, int inner, int* tile_m, int* tile_n, int* groups) {
+  const int f = gated_form(back ? PTDP_GEMM_NT : PTDP_GEMM_NN, rows, back ? inner : 2 * inner, width);
+  const SmallCost& c = kSmallCost[0][f >= 0 ? f : 0];
+  *tile_m = f >= 0 ? c.bm : kBM;
+  *tile_n = f >= 0 ? c.bn : kBN;
+  *groups = f >= 0 ? c.groups : 1;
 }
 // what the kernels address: operands below 2 GiB, rows of z below kWideRow
 bool gated_mlp_fits(int dtype, int rows, int width, int inner) {

@@ -89,19 +89,20 @@ def test_small(dtype, kind, rows, width, inner, bias):
 
 # the forms of the bf16 kernels: (forward, backward) tiles and groups of waves, asserted below
 FORMS = [(1998, 2048, 5504), (2048, 4096, 2816), (66, 512, 1368), (513, 1024, 1024), (700, 640, 4096), (300, 2000, 600), (1, 4096, 11008), (4000, 512, 512),
-         (1030, 4096, 4104), (129, 8192, 904), (64, 64, 16384), (2048, 1024, 1408), (520, 512, 2056), (1024, 3000, 2816), (16, 12288, 6144), (900, 200, 2400), (1500, 2328, 3168), (2048, 656, 6240)]
+         (1030, 4096, 4104), (129, 8192, 904), (64, 64, 16384), (2048, 1024, 1408), (520, 512, 2056), (1024, 3000, 2816), (16, 12288, 6144), (900, 200, 2400), (1500, 2328, 3168), (2048, 656, 6240),
+         (80, 472, 9000), (270, 392, 18000)]
 
 
-def form(mode, rows, cols, k):
+def form(back, rows, width, inner):
     v = [C.c_int() for _ in range(3)]
-    B.check(B.ptdp_gemm_form(mode, -(-rows // 8) * 8, cols, k, 0, 0, 0, 0, *[C.byref(x) for x in v]), "form")
+    B.check(B.ptdp_gated_mlp_form(back, rows, width, inner, *[C.byref(x) for x in v]), "form")
     return tuple(x.value for x in v)
 
 
 def test_every_form_is_run():
     every = {(256, 256, 1), (128, 128, 1), (128, 128, 2), (128, 64, 2), (64, 64, 2), (128, 64, 1), (256, 128, 2), (256, 192, 1)}
-    assert {form(B.GEMM_NN, r, 2 * i, w) for r, w, i in FORMS} == every
-    assert {form(B.GEMM_NT, r, i, w) for r, w, i in FORMS} == every
+    for back in (0, 1):
+        assert {form(back, *size) for size in FORMS} == every
 
 
 @gpu
@@ -198,4 +199,7 @@ def test_refusals():
     for null in ("dy", "w2", "z", "dz", "ws"):
         assert bwd(**{null: None}) == B.E_NULL_PTR
     assert B.ptdp_gated_mlp_workspace_bytes(B.BF16, 64, 60, 64) == 0 and B.ptdp_gated_mlp_workspace_bytes(B.BF16, 64, 64, 64) > 0
+    v = [C.byref(C.c_int()) for _ in range(3)]
+    assert B.ptdp_gated_mlp_form(0, 64, 64, 64, *v) == B.OK and B.ptdp_gated_mlp_form(2, 64, 64, 64, *v) == B.E_INVALID_ARG
+    assert B.ptdp_gated_mlp_form(1, 0, 64, 64, *v) == B.E_INVALID_ARG and B.ptdp_gated_mlp_form(1, 64, 64, 64, None, v[1], v[2]) == B.E_NULL_PTR
     assert fwd(dtype=B.F32, width=1 << 15, inner=1 << 13) == B.E_UNSUPPORTED and fwd(dtype=B.F32) == B.OK
