@@ -1028,7 +1028,7 @@ static int check_span_cfg(const ptdp_attn_span_cfg* c) {
   return attn_dh_supported(c->dtype, c->dh) && attn_span_fits(c) ? PTDP_OK : PTDP_E_UNSUPPORTED;
 }
 size_t ptdp_attn_span_workspace_bytes(const ptdp_attn_span_cfg* cfg) {
-  return check_span_cfg(cfg) == PTDP_OK ? align256((size_t)cfg->b * cfg->heads * cfg->s * sizeof(float)) : 0;
+  return check_span_cfg(cfg) == PTDP_OK ? align256(attn_span_stats_bytes(cfg)) : 0;
 }
 int ptdp_attn_span_fwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, void* ctx, float* lse, void* stream) {
   PTDP_TRY(check_span_cfg(cfg));
@@ -1044,7 +1044,7 @@ int ptdp_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const voi
   if (dqkv == qkv) return PTDP_E_INVALID_ARG;
   PTDP_TRY(check_aligned(qkv, spans, ctx, dctx, dqkv, workspace));
   if (cfg->s == 0 || cfg->b == 0) return PTDP_OK;
-  return launch_attn_span_bwd(cfg, qkv, spans, slopes, ctx, lse, dctx, dqkv, (float*)workspace, (hipStream_t)stream);
+  return launch_attn_span_bwd(cfg, qkv, spans, slopes, ctx, lse, dctx, dqkv, workspace, (hipStream_t)stream);
 }
 
 static int check_gated(int dtype, int gate, int rows, int width, int inner) {

@@ -147,20 +147,15 @@ constexpr float kLog2e = 1.4426950408889634f;
 struct SpanShape {
   int s, b, heads, kv_heads;
   float scale, cap;
-  const float* slopes;   // null: no bias
-};
-struct ScoreRule {
-  float mul, steep, bias;   // exponent of two per unit; 2 log2(e) scale / cap; units per key of distance
-  bool capped, biased;
-  __device__ __forceinline__ ScoreRule(const SpanShape& z, int head) {
-    capped = z.cap > 0.f;
-    mul = (capped ? z.cap : z.scale) * kLog2e;
-    steep = capped ? 2.f * kLog2e * z.scale / z.cap : 0.f;
-    bias = z.slopes ? z.slopes[head] * kLog2e / mul : 0.f;
-    biased = z.slopes != nullptr;
-  }
+  float mul, steep, per_slope;   // exponent of two per unit; 2 log2(e) scale / cap; units of bias per slope
+  const float* slopes;           // null: no bias
+  __device__ __forceinline__ bool capped() const { return cap > 0.f; }
+  bool capped_or_biased() const { return cap > 0.f || slopes; }
   // tanh with the hardware's exponential and reciprocal, as fast_tanh: absolute error 1e-7, of the cap
   __device__ __forceinline__ float tanh(float x) const { return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * steep)); }
+  __device__ __forceinline__ float bias(int head) const {   // units per key of distance, in a scalar register
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, slopes ? slopes[head] * per_slope : 0.f)));
+  }
 };
 // row r of a 32 x 32 accumulator, in rows of the lane's half
 constexpr int acc_row(int r) { return 8 * (r >> 2) + (r & 3); }
@@ -172,7 +167,8 @@ __device__ __forceinline__ void keep_span(f32x16_t& a, int from, uint32_t count,
 
 // A hidden weight is zero, but zero times an infinite or undefined element is not.  The kernels multiply as if all elements were
 // finite; where a sum comes out otherwise the workgroup walks again, and in tiles with hidden scores such elements enter the products as
-// zeros (finite_only) and are then added to the columns that see them.
+// zeros (finite_only) and are then added to the columns that see them.  (dK and dV have no registers for that: there a key with such a sum
+// is made again by itself.)
 __device__ __forceinline__ bool bf16_finite(uint32_t v) { return (v & 0x7f80u) != 0x7f80u; }
 __device__ __forceinline__ bf16x8_t finite_only(bf16x8_t v) {
   uint4 w = __builtin_bit_cast(uint4, v);
@@ -263,7 +259,7 @@ attn_span_fwd_kernel(const bf16_t* __restrict__ qkv, bf16_t* __restrict__ ctx, f
   };
   const int2 span = my_q < s ? span_of(view, j, my_q, s) : make_int2(kNoKey, 0);
   const uint32_t count = (uint32_t)max(span.y - span.x, 0);
-  const ScoreRule rule(z, e);
+  const float bias = z.bias(e);
   bf16x8_t qf[NKK];
 #pragma unroll
   for (int kk = 0; kk < NKK; ++kk) qf[kk] = frag_global(qb + (size_t)min(my_q, s - 1) * rs, my_q < s, kk, half);
@@ -301,18 +297,18 @@ attn_span_fwd_kernel(const bf16_t* __restrict__ qkv, bf16_t* __restrict__ ctx, f
         for (int sub = 0; sub < SUBS; ++sub) sacc[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fks.get(sub, kk), qf[kk], sacc[sub], 0, 0, 0);
       sched_reads_ahead<SUBS * NKK, 1>();
       __builtin_amdgcn_sched_barrier(0);
-      if (rule.capped) {
+      if (z.capped()) {
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[sub][r] = rule.tanh(sacc[sub][r]);
+          for (int r = 0; r < 16; ++r) sacc[sub][r] = z.tanh(sacc[sub][r]);
       }
-      if (rule.biased) {
+      if (z.slopes) {
         const float ahead = (float)(my_q - key0 - 4 * half);
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[sub][r] = fmaf(-rule.bias, fabsf(ahead - (float)(sub * 32 + acc_row(r))), sacc[sub][r]);
+          for (int r = 0; r < 16; ++r) sacc[sub][r] = fmaf(-bias, fabsf(ahead - (float)(sub * 32 + acc_row(r))), sacc[sub][r]);
       }
       if (!full) {
 #pragma unroll
@@ -327,7 +323,7 @@ attn_span_fwd_kernel(const bf16_t* __restrict__ qkv, bf16_t* __restrict__ ctx, f
       mx = fmaxf(mh.lo, mh.hi);
       const float ref = mx == -INFINITY ? 0.f : mx;   // no key of the row so far: weights of zero, not exp(-inf + inf)
       if (__any(mx > m_run)) {   // some row's maximum moved: rescale what has been accumulated
-        const float corr = __builtin_amdgcn_exp2f((m_run - ref) * rule.mul);
+        const float corr = __builtin_amdgcn_exp2f((m_run - ref) * z.mul);
         m_run = mx;
         l_run *= corr;
 #pragma unroll
@@ -335,12 +331,12 @@ attn_span_fwd_kernel(const bf16_t* __restrict__ qkv, bf16_t* __restrict__ ctx, f
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[d][r] *= corr;
       }
-      const float mc = ref * rule.mul;
+      const float mc = ref * z.mul;
       bf16x8_t pf[SUBS][2], vr[2][NDT];
       auto weights = [&](int sub) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          sacc[sub][r] = __builtin_amdgcn_exp2f(sacc[sub][r] * rule.mul - mc);
+          sacc[sub][r] = __builtin_amdgcn_exp2f(sacc[sub][r] * z.mul - mc);
           l_run += sacc[sub][r];
         }
         pf[sub][0] = pack_frag(sacc[sub], 0);
@@ -404,7 +400,7 @@ attn_span_fwd_kernel(const bf16_t* __restrict__ qkv, bf16_t* __restrict__ ctx, f
     __syncthreads();
     if (grp == 1) return;
     const float m1 = part[0], l1 = part[64], m = fmaxf(m_run, m1), ref = m == -INFINITY ? 0.f : m;
-    const float a0 = __builtin_amdgcn_exp2f((m_run - ref) * rule.mul), a1 = __builtin_amdgcn_exp2f((m1 - ref) * rule.mul);
+    const float a0 = __builtin_amdgcn_exp2f((m_run - ref) * z.mul), a1 = __builtin_amdgcn_exp2f((m1 - ref) * z.mul);
     l_run = l_run * a0 + l1 * a1;
     m_run = m;
 #pragma unroll
@@ -414,13 +410,13 @@ attn_span_fwd_kernel(const bf16_t* __restrict__ qkv, bf16_t* __restrict__ ctx, f
   }
   if (my_q < s) {
     store_cols<NDT>(ctx + ((size_t)my_q * b + j) * z.heads * DH + (size_t)e * DH, o, count ? 1.f / l_run : 0.f, half);
-    if (half == 0) lse[((size_t)j * z.heads + e) * s + my_q] = count ? m_run * (rule.mul / kLog2e) + __logf(l_run) : -INFINITY;
+    if (half == 0) lse[((size_t)j * z.heads + e) * s + my_q] = count ? m_run * (z.mul / kLog2e) + __logf(l_run) : -INFINITY;
   }
 }
 
 // ------------------------------------------------------------------------------------------------
-// Backward, bf16.  dQ: a workgroup owns 32 QW queries and walks their keys as the forward kernel does; it also writes D = dctx.ctx, which
-// the dK/dV kernel, launched next, reads.  ctx has been rounded to bf16, and where a softmax is sharp dp - D is a small difference: D
+// Backward, bf16.  dQ: a workgroup owns 32 QW queries and walks their keys as the forward kernel does; it also writes every query's
+// lse log2(e) (infinite where nothing is seen) and D = dctx.ctx, which the dK/dV kernel, launched next, reads.  ctx has been rounded to bf16, and where a softmax is sharp dp - D is a small difference: D
 // from it is off by up to 2^-8 |dctx| |ctx| / sqrt(dh).  The rows' sums of p (dp - D), zero by definition, tell by how much: what dK gets
 // is the corrected D, and walks of up to kSpanTwice tiles, whose few keys average least out, are made once more with it (dQ's
 // relative error against 64 bits with a row's D as it is, s = 2, 8, 100, 2048: 3.9e-3, 4.3e-3, 2.9e-3, 2.6e-3; two roundings alone 2.3e-3).
@@ -429,7 +425,7 @@ constexpr int kSpanTwice = 2;
 template <int DH, int QW, int NP, int KT>
 __global__ void __launch_bounds__(64 * QW * NP, 2)
 attn_span_dq_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ ctx, const bf16_t* __restrict__ dctx, const float* __restrict__ lse,
-                    float* __restrict__ delta, bf16_t* __restrict__ dqkv, SpanView view, SpanShape z) {
+                    float2* __restrict__ stats, bf16_t* __restrict__ dqkv, SpanView view, SpanShape z) {
   constexpr int NKK = DH / 16, NDT = DH / 32, SUBS = KT / 32;
   constexpr uint32_t kTile = TileDma<DH, QW, KT, false>::kBytes, kStage = 2 * kTile;
   extern __shared__ __attribute__((aligned(1024))) char smem_all[];
@@ -455,7 +451,7 @@ attn_span_dq_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ c
   };
   const int2 span = valid ? span_of(view, j, my_q, s) : make_int2(kNoKey, 0);
   const uint32_t count = (uint32_t)max(span.y - span.x, 0);
-  const ScoreRule rule(z, e);
+  const float bias = z.bias(e);
   const size_t stat = ((size_t)j * z.heads + e) * s + my_q;
   const float L2 = count ? lse[stat] * kLog2e : INFINITY;   // an empty span: weights of zero
   bf16x8_t qf[NKK], dof[NKK];
@@ -499,25 +495,25 @@ attn_span_dq_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ c
         sched_reads_ahead<2 * NKK, 1>();
         __builtin_amdgcn_sched_barrier(0);
         const float ahead = (float)(my_q - key0 - sub * 32 - 4 * half);
-        if (rule.capped) {
+        if (z.capped()) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float th = rule.tanh(sacc[r]), t = fmaf(-rule.bias, fabsf(ahead - (float)acc_row(r)), th);
-            sacc[r] = __builtin_amdgcn_exp2f(t * rule.mul - L2) * (dp[r] - D);
+            const float th = z.tanh(sacc[r]), t = fmaf(-bias, fabsf(ahead - (float)acc_row(r)), th);
+            sacc[r] = __builtin_amdgcn_exp2f(t * z.mul - L2) * (dp[r] - D);
             dp[r] = fmaf(-th, th, 1.f);
           }
         } else {
-          if (rule.biased) {
+          if (z.slopes) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sacc[r] = fmaf(-rule.bias, fabsf(ahead - (float)acc_row(r)), sacc[r]);
+            for (int r = 0; r < 16; ++r) sacc[r] = fmaf(-bias, fabsf(ahead - (float)acc_row(r)), sacc[r]);
           }
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(sacc[r] * rule.mul - L2) * (dp[r] - D);
+          for (int r = 0; r < 16; ++r) sacc[r] = __builtin_amdgcn_exp2f(sacc[r] * z.mul - L2) * (dp[r] - D);
         }
         if (!full) keep_span(sacc, span.x - key0 - sub * 32 - 4 * half, count, 0.f);
 #pragma unroll
         for (int r = 0; r < 16; ++r) over += sacc[r];
-        if (rule.capped) {
+        if (z.capped()) {
           if (!full) keep_span(dp, span.x - key0 - sub * 32 - 4 * half, count, 0.f);   // (zero times a hidden NaN)
 #pragma unroll
           for (int r = 0; r < 16; ++r) sacc[r] *= dp[r];
@@ -565,7 +561,7 @@ attn_span_dq_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ c
     walk(std::true_type{});
     miss = missing();
   }
-  if (grp == 0 && half == 0 && valid) delta[stat] = D + miss;
+  if (grp == 0 && half == 0 && valid) stats[stat] = make_float2(L2, D + miss);
   if constexpr (NP > 1) {
     // the second group's sums join the first's: register r of lane l of wave w at sum[w][r][l]
     float* sum = reinterpret_cast<float*>(smem_all) + wave * (NDT * 16 * 64) + lane;
@@ -586,26 +582,98 @@ attn_span_dq_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ c
   if (valid) store_cols<NDT>(dqkv + (size_t)my_q * rs + j * row + (size_t)e * DH, acc, z.scale, half);
 }
 
+// QT queries' eight bytes each from `from` to LDS, zeros from `bytes` on: lane i's four bytes land at lds + 4 i (assembly as attn_load_lds)
+template <int QT> __device__ __forceinline__ void span_load_rows(const void* from, int bytes, uint32_t lds, int lane) {
+  const uint64_t a = reinterpret_cast<uint64_t>(from);
+  const attn_rsrc_t r = {(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, bytes > 0 ? (uint32_t)bytes : 0u, 0x00020000u};
+#pragma unroll
+  for (int i = 0; i < QT / 32; ++i)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds + i * 256), "v"(i * 256 + lane * 4), "s"(r) : "memory", "m0");
+}
+
 // dK, dV of 32 KW keys of a key/value head: the queries of the group's heads that may see them, head after head, stream through two LDS
-// stages of QT queries; their lse, D and spans travel in registers and are written to the next stage behind the arithmetic.
+// stages of QT queries, with their statistics (lse, D) and spans, all of it straight from memory.  Nothing of the next tile passes through
+// vector registers: both results, K and V leave none over.
 // SPLIT: KW waves compute S, dP and dK and KW waves S and dV (heads of 160: both results do not fit two waves' registers).
 template <int DH, int KW, int NP, int QT, bool SPLIT> struct SpanDkvGeom {
   static constexpr int kWaves = SPLIT ? 2 * KW : KW, kThreads = 64 * kWaves;   // of a group
-  static constexpr int kTile = QT * DH * 2, kStats = 2 * kTile, kStage = kStats + 4 * QT * (int)sizeof(float);
+  static constexpr int kTile = QT * DH * 2, kStats = 2 * kTile, kSpans = kStats + 8 * QT, kStage = kSpans + 8 * QT;
   static constexpr int kSums = NP > 1 ? KW * 2 * (DH / 2) * 64 * (int)sizeof(float) : 0;
   static constexpr int kBytes = NP * 2 * kStage > kSums ? NP * 2 * kStage : kSums;
 };
-template <int DH, int KW, int NP, int QT, bool SPLIT>
+struct SpanDkvArgs {
+  const bf16_t *qkv, *dctx;
+  const float2* stats;
+  bf16_t* dqkv;
+  SpanView view;
+  SpanShape z;
+};
+// A key whose dV or dK has a sum that is not finite (`want`: bit 0, bit 1) is made again from the queries that see it and from no others, an
+// element to a lane and query after query: a hidden query's zero weight times what is not finite may have got in.  It reads the kernel's
+// arguments from where the launch left them and is not inlined: kept for it, they would take the kernel's registers.
+template <int DH> __device__ __attribute__((noinline)) void span_dkv_again(const SpanDkvArgs& a, int key, int kve, int j, int want) {
+  const SpanShape& z = a.z;
+  const int s = z.s, group = z.heads / z.kv_heads, lane = threadIdx.x & 63;
+  const size_t row = (size_t)(z.heads + 2 * z.kv_heads) * DH, rs = z.b * row, dors = (size_t)z.b * z.heads * DH;
+  const bf16_t *sample = a.qkv + j * row, *kr = sample + (size_t)key * rs + (size_t)(z.heads + kve) * DH, *vr = kr + (size_t)z.kv_heads * DH;
+  constexpr int NE = (DH + 63) / 64;
+  auto element = [&](const bf16_t* from, int i) { return 64 * i + lane < DH ? bf16_to_f32(from[64 * i + lane]) : 0.f; };
+  float ke[NE], ve[NE], dk[NE], dv[NE];
+#pragma unroll
+  for (int i = 0; i < NE; ++i) {
+    ke[i] = element(kr, i);
+    ve[i] = element(vr, i);
+    dk[i] = dv[i] = 0.f;
+  }
+#pragma unroll 1
+  for (int head = kve * group; head < (kve + 1) * group; ++head) {
+    const float bias = z.bias(head);
+    const float2* st = a.stats + ((size_t)j * z.heads + head) * s;
+#pragma unroll 1
+    for (int q = 0; q < s; ++q) {
+      const int2 x = span_of(a.view, j, q, s);
+      if (!((uint32_t)(key - x.x) < (uint32_t)(x.y - x.x))) continue;
+      const bf16_t *qr = sample + (size_t)q * rs + (size_t)head * DH, *dr = a.dctx + (size_t)q * dors + ((size_t)j * z.heads + head) * DH;
+      float qe[NE], de[NE], qk = 0.f, dp = 0.f;
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        qe[i] = element(qr, i);
+        de[i] = element(dr, i);
+        qk = fmaf(qe[i], ke[i], qk);
+        dp = fmaf(de[i], ve[i], dp);
+      }
+      qk = wave_sum(qk);
+      dp = wave_sum(dp);
+      const float th = z.capped() ? z.tanh(qk) : qk, p = __builtin_amdgcn_exp2f(fmaf(-bias, fabsf((float)(q - key)), th) * z.mul - st[q].x);
+      const float ds = p * (dp - st[q].y) * (z.capped() ? fmaf(-th, th, 1.f) : 1.f);
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        dv[i] = fmaf(p, de[i], dv[i]);
+        dk[i] = fmaf(ds, qe[i], dk[i]);
+      }
+    }
+  }
+  bf16_t* to = a.dqkv + (kr - a.qkv);
+#pragma unroll
+  for (int i = 0; i < NE; ++i) {
+    if (64 * i + lane >= DH) continue;
+    if (want & 2) to[64 * i + lane] = f32_to_bf16(dk[i] * z.scale);
+    if (want & 1) to[(size_t)z.kv_heads * DH + 64 * i + lane] = f32_to_bf16(dv[i]);
+  }
+}
+// SCORED: there may be a cap or a bias (without that code heads of 160 fit their registers).
+template <int DH, int KW, int NP, int QT, bool SPLIT, bool SCORED>
 __global__ void __launch_bounds__(64 * KW * (SPLIT ? 2 : 1) * NP, 2)
-attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dctx, const float* __restrict__ lse, const float* __restrict__ delta,
-                     bf16_t* __restrict__ dqkv, SpanView view, SpanShape z) {
+attn_span_dkv_kernel(SpanDkvArgs a) {
+  const SpanView view = a.view;
+  const SpanShape& z = a.z;
   using Geom = SpanDkvGeom<DH, KW, NP, QT, SPLIT>;
   constexpr int NKK = DH / 16, NDT = DH / 32, kKeys = 32 * KW, SUBS = QT / 32, GW = Geom::kWaves, kTile = Geom::kTile, kStage = Geom::kStage;
   constexpr int NR = SPLIT ? 1 : 2;   // results of a wave
   extern __shared__ __attribute__((aligned(1024))) char smem_all[];
   const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = NP == 1 ? 0 : wave_all / GW, wave = wave_all % GW;
-  const int kw = wave % KW, tid = threadIdx.x & (Geom::kThreads - 1);
-  static_assert((Geom::kThreads & (Geom::kThreads - 1)) == 0 && QT <= Geom::kThreads);
+  const int kw = wave % KW;
+  static_assert(GW > 1);
   char* smem = smem_all + grp * 2 * kStage;
   const uint32_t lds0 = attn_lds_offset(smem);
   const int s = z.s, b = z.b, nkb = (s + kKeys - 1) / kKeys, group = z.heads / z.kv_heads;
@@ -616,17 +684,18 @@ attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ 
   const bool want_dk = !SPLIT || ((wave / KW) ^ (NP == 2 ? grp : (int)(blockIdx.x >> 8))) & 1;
   const int lane = threadIdx.x & 63, half = lane >> 5, l31 = lane & 31;
   const size_t row = (size_t)(z.heads + 2 * z.kv_heads) * DH, rs = b * row, orow = (size_t)z.heads * DH, dors = b * orow;
-  const bf16_t* sample = qkv + j * row;
+  const bf16_t* sample = a.qkv + j * row;
   const bf16_t *kb = sample + (size_t)(z.heads + kve) * DH, *vb = kb + (size_t)z.kv_heads * DH;
-  const bf16_t *qb = sample + (size_t)kve * group * DH, *dob = dctx + j * orow + (size_t)kve * group * DH;
+  const bf16_t *qb = sample + (size_t)kve * group * DH, *dob = a.dctx + j * orow + (size_t)kve * group * DH;
   const size_t stat0 = ((size_t)j * z.heads + (size_t)kve * group) * s;
   const int key_blk = kblk * kKeys, key_first = key_blk + kw * 32, my_key = key_first + l31;
   const bool valid = my_key < s;
 
   // the tiles of queries that may see a key of the block: from the first to the last block of 32 queries whose bounds meet it
   int qt_first = key_blk / QT, qt_end = (s + QT - 1) / QT;
+  const int nt = (s + kSpanRows - 1) / kSpanRows;
+  const SpanBounds* bounds = view.bounds + (size_t)j * nt;   // (read if there are spans)
   if (view.range) {
-    const int nt = (s + kSpanRows - 1) / kSpanRows;
     int* found = reinterpret_cast<int*>(smem_all);
     if (threadIdx.x == 0) {
       found[0] = kNoKey;
@@ -634,7 +703,7 @@ attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ 
     }
     __syncthreads();
     for (int t = threadIdx.x; t < nt; t += blockDim.x) {
-      const SpanBounds y = view.bounds[(size_t)j * nt + t];
+      const SpanBounds y = bounds[t];
       if (y.first < key_blk + kKeys && y.last > key_blk) {
         atomicMin(&found[0], t);
         atomicMax(&found[1], t);
@@ -655,39 +724,32 @@ attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ 
   dma_q.init(rs, lane);
   dma_do.init(dors, lane);
   struct Place { int head, qt; };   // of the group; the tile
-  auto advance = [&](Place p) {
-    p.qt += NP;
+  auto settle = [&](Place p) {
     while (p.qt >= qt_end) {
       p.qt -= nq;
       ++p.head;
     }
     return p;
   };
-  float lse_r = 0.f, delta_r = 0.f;
-  int2 span_r = make_int2(kNoKey, 0);
-  SpanBounds next = {kNoKey, 0, 0, kNoKey};
   auto request = [&](Place p, uint32_t at) {
     if (GW == DW || wave < DW) dma_q.issue(qb + (size_t)p.head * DH, p.qt * QT, s, lds0 + at, wave % DW);
     if (GW == DW || wave >= DW) dma_do.issue(dob + (size_t)p.head * DH, p.qt * QT, s, lds0 + at + kTile, wave % DW);
+    // eight bytes a query, zeros past the end
+    const int q = p.qt * QT, bytes = min(QT, s - q) * 8;
+    if (wave == 0) span_load_rows<QT>(a.stats + stat0 + (size_t)p.head * s + q, bytes, lds0 + at + Geom::kStats, lane);
+    if (wave == 1 && view.range) span_load_rows<QT>(view.range + (size_t)j * s + q, bytes, lds0 + at + Geom::kSpans, lane);
   };
-  auto fetch = [&](Place p) {
-    const int q = p.qt * QT + tid;
-    if (tid < QT) {
-      const size_t at = stat0 + (size_t)p.head * s + min(q, s - 1);
-      span_r = q < s ? span_of(view, j, q, s) : make_int2(kNoKey, 0);
-      lse_r = span_r.y > span_r.x ? lse[at] * kLog2e : INFINITY;   // p is zero past the end and where nothing is seen
-      delta_r = q < s ? delta[at] : 0.f;
+  // the tile's bounds and bias, from scalar loads: they are a tile's to wait for, not a lane's
+  typedef __attribute__((address_space(4))) const int scalar_int_t;
+  auto bounds_of_tile = [&](Place p) {
+    if (!view.range) return SpanBounds{0, min(s, (p.qt + 1) * QT), 0, p.qt * QT + 1};
+    SpanBounds x = {kNoKey, 0, 0, kNoKey};
+#pragma unroll
+    for (int i = 0; i < SUBS; ++i) {   // (a block past the last one is the last one again)
+      const scalar_int_t* y = (scalar_int_t*)(bounds + min(p.qt * SUBS + i, nt - 1));
+      x = {min(x.first, y[0]), max(x.last, y[1]), max(x.inner_lo, y[2]), min(x.inner_hi, y[3])};
     }
-    next = bounds_of(view, j, p.qt * SUBS, SUBS, s);
-  };
-  auto put = [&](uint32_t at) {
-    if (tid < QT) {
-      float* st = reinterpret_cast<float*>(smem + at + Geom::kStats);
-      st[tid] = lse_r;
-      st[QT + tid] = delta_r;
-      st[2 * QT + tid] = __int_as_float(span_r.x);
-      st[3 * QT + tid] = __int_as_float(max(span_r.y - span_r.x, 0));
-    }
+    return x;
   };
   bf16x8_t kf[NKK], vf[NKK];
 #pragma unroll
@@ -701,17 +763,11 @@ attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ 
   t0.init(lds0, lane);
   f32x16_t acc[NR][NDT];   // dV and dK, or one of them
 
-  auto walk = [&](auto careful) {   // careful: see add_nonfinite
-    constexpr bool CAREFUL = decltype(careful)::value;
+  {
     Place at = {0, qt_first + grp};
-    while (nq > 0 && at.qt >= qt_end) {
-      at.qt -= nq;
-      ++at.head;
-    }
+    if (nq > 0) at = settle(at);
     if (nq > 0 && at.head < group) {
       request(at, 0);
-      fetch(at);
-      put(0);
     }
 #pragma unroll
     for (int r = 0; r < NR; ++r)
@@ -722,22 +778,18 @@ attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ 
 #pragma unroll 1
     for (int step = 0; step < steps; ++step) {
       const int q0 = at.qt * QT, head = at.head;
-      const bool mine = head < group;
-      const SpanBounds bnd = next;
+      const SpanBounds bnd = bounds_of_tile(at);
+      const float bias = SCORED && z.slopes ? ((__attribute__((address_space(4))) const float*)z.slopes)[min(kve * group + head, z.heads - 1)] * z.per_slope : 0.f;
       attn_tiles_ready();
-      const Place then = advance(at);
+      const Place then = settle({at.head, at.qt + NP});
       const bool more = then.head < group;
       const uint32_t other = stage == 0 ? kStage : 0;
-      if (more) {
-        fetch(then);
-        request(then, other);
-      }
+      if (more) request(then, other);
       // (skipped if no key of the wave exists or no query of the tile sees one)
-      if (mine && key_first < s && bnd.first < key_first + 32 && bnd.last > key_first) {
-        const ScoreRule rule(z, kve * group + head);
+      if (head < group && key_first < s && bnd.first < key_first + 32 && bnd.last > key_first) {
         const FragDirect<QT> fs = f0.at(stage);
         const FragTr<QT> ts = t0.at(stage);
-        const char* stats = smem + stage + Geom::kStats;
+        const char *rows = smem + stage + Geom::kStats, *spans = smem + stage + Geom::kSpans;
         const bool full = bnd.inner_lo <= key_first && bnd.inner_hi >= key_first + 32;
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
@@ -756,72 +808,63 @@ attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ 
           }
           __builtin_amdgcn_sched_barrier(0);
           const float ahead = (float)(my_key - q0 - sub * 32 - 4 * half);
-          if (rule.biased && !rule.capped) {
+          if (SCORED && z.slopes && !z.capped()) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sacc[r] = fmaf(-rule.bias, fabsf(ahead - (float)acc_row(r)), sacc[r]);
+            for (int r = 0; r < 16; ++r) sacc[r] = fmaf(-bias, fabsf(ahead - (float)acc_row(r)), sacc[r]);
           }
-          if (rule.capped) {
+          if (SCORED && z.capped()) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-              const int ql = sub * 32 + 8 * g + 4 * half;   // local index of the first of 4 consecutive queries
-              const f32x4_t Ls = *reinterpret_cast<const f32x4_t*>(stats + ql * 4), Ds = *reinterpret_cast<const f32x4_t*>(stats + (QT + ql) * 4);
+              const char* four = rows + (sub * 32 + 8 * g + 4 * half) * 8;   // lse and D of four consecutive queries
+              const f32x4_t two[2] = {*reinterpret_cast<const f32x4_t*>(four), *reinterpret_cast<const f32x4_t*>(four + 16)};
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const int r = 4 * g + i;
-                const float th = rule.tanh(sacc[r]), p = __builtin_amdgcn_exp2f(fmaf(-rule.bias, fabsf(ahead - (float)acc_row(r)), th) * rule.mul - Ls[i]);
+                const float th = z.tanh(sacc[r]), p = __builtin_amdgcn_exp2f(fmaf(-bias, fabsf(ahead - (float)acc_row(r)), th) * z.mul - two[i >> 1][2 * (i & 1)]);
                 sacc[r] = p;
-                dp[r] = p * (dp[r] - Ds[i]) * fmaf(-th, th, 1.f);
+                dp[r] = p * (dp[r] - two[i >> 1][2 * (i & 1) + 1]) * fmaf(-th, th, 1.f);
               }
             }
           } else {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-              const int ql = sub * 32 + 8 * g + 4 * half;
-              const f32x4_t Ls = *reinterpret_cast<const f32x4_t*>(stats + ql * 4), Ds = *reinterpret_cast<const f32x4_t*>(stats + (QT + ql) * 4);
+              const char* four = rows + (sub * 32 + 8 * g + 4 * half) * 8;
+              const f32x4_t two[2] = {*reinterpret_cast<const f32x4_t*>(four), *reinterpret_cast<const f32x4_t*>(four + 16)};
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const int r = 4 * g + i;
-                const float p = __builtin_amdgcn_exp2f(sacc[r] * rule.mul - Ls[i]);
+                const float p = __builtin_amdgcn_exp2f(sacc[r] * z.mul - two[i >> 1][2 * (i & 1)]);
                 sacc[r] = p;
-                dp[r] = p * (dp[r] - Ds[i]);
+                dp[r] = p * (dp[r] - two[i >> 1][2 * (i & 1) + 1]);
               }
             }
           }
           if (!full) {
             typedef int i32x4_t __attribute__((ext_vector_type(4)));
+            if (view.range) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const int ql = sub * 32 + 8 * g + 4 * half;
-              const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(stats + (2 * QT + ql) * 4), n = *reinterpret_cast<const i32x4_t*>(stats + (3 * QT + ql) * 4);
+              for (int g = 0; g < 4; ++g) {
+                const char* four = spans + (sub * 32 + 8 * g + 4 * half) * 8;
+                const i32x4_t two[2] = {*reinterpret_cast<const i32x4_t*>(four), *reinterpret_cast<const i32x4_t*>(four + 16)};
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const bool seen = (uint32_t)(my_key - lo[i]) < (uint32_t)n[i];
-                sacc[4 * g + i] = seen ? sacc[4 * g + i] : 0.f;
-                dp[4 * g + i] = seen ? dp[4 * g + i] : 0.f;
+                for (int i = 0; i < 4; ++i) {   // (an empty span, {kNoKey, 0}, has no key either: no key is as far from kNoKey as 0 is)
+                  const int lo = two[i >> 1][2 * (i & 1)], hi = two[i >> 1][2 * (i & 1) + 1];
+                  const bool seen = (uint32_t)(my_key - lo) < (uint32_t)(hi - lo);
+                  sacc[4 * g + i] = seen ? sacc[4 * g + i] : 0.f;
+                  dp[4 * g + i] = seen ? dp[4 * g + i] : 0.f;
+                }
+              }
+            } else {
+              const int before = my_key - q0 - sub * 32 - 4 * half;   // local queries below it precede my_key
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                sacc[r] = acc_row(r) < before ? 0.f : sacc[r];
+                dp[r] = acc_row(r) < before ? 0.f : dp[r];
               }
             }
           }
           const bf16x8_t pf[2] = {pack_frag(sacc, 0), pack_frag(sacc, 1)}, dsf[2] = {pack_frag(dp, 0), pack_frag(dp, 1)};
-          if (CAREFUL && !full) {
-            const int first = q0 + sub * 32;
-            auto seen = [&](int r) {
-              const int2 x = span_of(view, j, first + r, s);
-              return (uint32_t)(my_key - x.x) < (uint32_t)max(x.y - x.x, 0);
-            };
-#pragma unroll
-            for (int x = 0; x < NR; ++x) {   // dV (x = 0), dK; SPLIT: the wave's own
-              const bool dk = SPLIT ? want_dk : x == 1;
-              const uint32_t tile = dk ? 0 : kTile;
-              const FragTr<QT> tw{ts.lo + tile, ts.hi + tile};
-#pragma unroll
-              for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-                for (int d = 0; d < NDT; ++d)
-                  acc[x][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_only(tw.get(d, sub, ks)), dk ? dsf[ks] : pf[ks], acc[x][d], 0, 0, 0);
-              const f32x16_t w[1] = {dk ? dp : sacc};
-              add_nonfinite<NDT, 1>(acc[x], w, (dk ? qb : dob) + (size_t)head * DH, dk ? rs : dors, first, s, lane, seen);
-            }
-          } else if constexpr (SPLIT) {
+          if constexpr (SPLIT) {
             // Q^T or dO^T; P or dS
             const uint32_t tile = want_dk ? 0 : kTile;
             const FragTr<QT> tw{ts.lo + tile, ts.hi + tile};
@@ -843,15 +886,10 @@ attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ 
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      if (more) put(other);
       at = then;
       stage = other;
     }
-  };
-  walk(std::false_type{});
-  bool good = all_finite(acc[0]);
-  if constexpr (NR == 2) good = good && all_finite(acc[1]);
-  if (any_of_workgroup(!good, reinterpret_cast<int*>(smem_all))) walk(std::true_type{});
+  }
   if constexpr (NP > 1) {
     // the second group's sums join the first's: register r of lane l of the wave with keys kw (and one result) at sum[..][r][l]
     float* sum = reinterpret_cast<float*>(smem_all) + (SPLIT ? (want_dk ? KW : 0) + kw : 2 * kw) * (NDT * 16 * 64) + lane;
@@ -873,15 +911,20 @@ attn_span_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ 
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[x][d][r] += sum[((x * NDT + d) * 16 + r) * 64];
   }
-  if (valid) {
-    bf16_t* dk = dqkv + (size_t)my_key * rs + j * row + (size_t)(z.heads + kve) * DH;
-    bf16_t* dv = dk + (size_t)z.kv_heads * DH;
-    if constexpr (SPLIT) {
-      store_cols<NDT>(want_dk ? dk : dv, acc[0], want_dk ? z.scale : 1.f, half);
-    } else {
-      store_cols<NDT>(dv, acc[0], 1.f, half);
-      store_cols<NDT>(dk, acc[1], z.scale, half);
-    }
+  bf16_t* out = a.dqkv + (size_t)my_key * rs + j * row + (size_t)(z.heads + kve) * DH;   // dK; dV kv_heads further on
+  uint64_t bad[2] = {0, 0};   // keys whose dV, dK has a sum that is not finite
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    const bool dk = SPLIT ? want_dk : x == 1;
+    const uint64_t m = __ballot(valid && !all_finite(acc[x])), either = (m | m >> 32) & 0xffffffffu;
+    if (valid && !(either >> l31 & 1)) store_cols<NDT>(out + (dk ? 0 : (size_t)z.kv_heads * DH), acc[x], dk ? z.scale : 1.f, half);
+    bad[dk ? 1 : 0] = either;
+  }
+  const SpanDkvArgs* kernargs = (const SpanDkvArgs*)(const char*)__builtin_amdgcn_kernarg_segment_ptr();   // (only a kernel knows the place)
+#pragma unroll 1
+  for (uint64_t left = bad[0] | bad[1]; left; left &= left - 1) {
+    const int k = __ffsll((unsigned long long)left) - 1;
+    span_dkv_again<DH>(*kernargs, key_first + k, kve, j, (int)(bad[0] >> k & 1) | (int)(bad[1] >> k & 1) << 1);
   }
 }
 
@@ -1130,7 +1173,12 @@ bool attn_span_fits(const ptdp_attn_span_cfg* c) {
   if (c->dtype == PTDP_F32) return c->heads <= 65535 && c->b <= 65535 && pitch < (1ull << 31);
   return pairs < (1ull << 31) && attn_slice_fits(pitch, c->dh) && attn_grid_levels((c->s + 63) / 64, c->heads, c->b) < (1ll << 32) / 512;
 }
-static SpanShape span_shape(const ptdp_attn_span_cfg* c, const float* slopes) { return {c->s, c->b, c->heads, c->kv_heads, c->scale, c->cap, slopes}; }
+static SpanShape span_shape(const ptdp_attn_span_cfg* c, const float* slopes) {
+  const bool capped = c->cap > 0.f;
+  const float mul = (capped ? c->cap : c->scale) * kLog2e;
+  return {c->s, c->b, c->heads, c->kv_heads, c->scale, c->cap, mul, capped ? 2.f * kLog2e * c->scale / c->cap : 0.f, kLog2e / mul, slopes};
+}
+size_t attn_span_stats_bytes(const ptdp_attn_span_cfg* c) { return (size_t)c->b * c->heads * c->s * sizeof(float2); }   // fp32: D alone
 // the square's visible part is not known to the host: counted as the causal half
 static double span_flops(const ptdp_attn_span_cfg* c) { return 2.0 * c->b * c->heads * (double)c->s * c->s * c->dh; }
 
@@ -1146,7 +1194,7 @@ static int span_fwd_t(const bf16_t* qkv, bf16_t* ctx, float* lse, const SpanView
   return PTDP_OK;
 }
 template <int DH, int QW, int NP, int KT>
-static int span_dq_t(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, const float* lse, float* delta, bf16_t* dqkv, const SpanView& view,
+static int span_dq_t(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, const float* lse, float2* stats, bf16_t* dqkv, const SpanView& view,
                      const SpanShape& z, hipStream_t st) {
   constexpr int tiles = NP * 4 * TileDma<DH, QW, KT, false>::kBytes, sums = NP > 1 ? QW * (DH / 2) * 64 * (int)sizeof(float) : 0;
   constexpr int smem = tiles > sums ? tiles : sums;
@@ -1154,19 +1202,24 @@ static int span_dq_t(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, c
   const auto kernel = attn_span_dq_kernel<DH, QW, NP, KT>;
   if (set_dynamic_smem(reinterpret_cast<const void*>(kernel), smem, done) != PTDP_OK) return PTDP_E_HIP;
   const dim3 grid(attn_grid_levels((z.s + 32 * QW - 1) / (32 * QW), z.heads, z.b));
-  hipLaunchKernelGGL(kernel, grid, dim3(64 * QW * NP), smem, st, qkv, ctx, dctx, lse, delta, dqkv, view, z);
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * QW * NP), smem, st, qkv, ctx, dctx, lse, stats, dqkv, view, z);
   return PTDP_OK;
 }
-template <int DH, int KW, int NP, int QT, bool SPLIT>
-static int span_dkv_t(const bf16_t* qkv, const bf16_t* dctx, const float* lse, const float* delta, bf16_t* dqkv, const SpanView& view,
+template <int DH, int KW, int NP, int QT, bool SPLIT, bool SCORED>
+static int span_dkv_scored_t(const bf16_t* qkv, const bf16_t* dctx, const float2* stats, bf16_t* dqkv, const SpanView& view,
                       const SpanShape& z, hipStream_t st) {
   using Geom = SpanDkvGeom<DH, KW, NP, QT, SPLIT>;
   static once_flag_t done[kMaxDevices];
-  const auto kernel = attn_span_dkv_kernel<DH, KW, NP, QT, SPLIT>;
+  const auto kernel = attn_span_dkv_kernel<DH, KW, NP, QT, SPLIT, SCORED>;
   if (set_dynamic_smem(reinterpret_cast<const void*>(kernel), Geom::kBytes, done) != PTDP_OK) return PTDP_E_HIP;
   const dim3 grid(attn_grid_levels((z.s + 32 * KW - 1) / (32 * KW), z.kv_heads, z.b));
-  hipLaunchKernelGGL(kernel, grid, dim3(Geom::kThreads * NP), Geom::kBytes, st, qkv, dctx, lse, delta, dqkv, view, z);
+  hipLaunchKernelGGL(kernel, grid, dim3(Geom::kThreads * NP), Geom::kBytes, st, SpanDkvArgs{qkv, dctx, stats, dqkv, view, z});
   return PTDP_OK;
+}
+template <int DH, int KW, int NP, int QT, bool SPLIT>
+static int span_dkv_t(const bf16_t* qkv, const bf16_t* dctx, const float2* stats, bf16_t* dqkv, const SpanView& view, const SpanShape& z, hipStream_t st) {
+  return z.capped_or_biased() ? span_dkv_scored_t<DH, KW, NP, QT, SPLIT, true>(qkv, dctx, stats, dqkv, view, z, st)
+                              : span_dkv_scored_t<DH, KW, NP, QT, SPLIT, false>(qkv, dctx, stats, dqkv, view, z, st);
 }
 static long long span_blocks(int s, int heads, int b) { return (long long)((s + 63) / 64) * heads * b; }   // of 64 rows
 
@@ -1175,19 +1228,23 @@ template <int DH> static int span_fwd_dh(const bf16_t* qkv, bf16_t* ctx, float* 
   return span_fwd_t<DH, 4, 1, 64>(qkv, ctx, lse, view, z, st);
 }
 template <int DH>
-static int span_bwd_dh(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, const float* lse, float* delta, bf16_t* dqkv, const SpanView& view,
+static int span_bwd_dh(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, const float* lse, float2* stats, bf16_t* dqkv, const SpanView& view,
                        const SpanShape& z, hipStream_t st) {
   const long long ncu = attn_compute_units();
-  const int rc = span_blocks(z.s, z.heads, z.b) <= 3 * ncu ? span_dq_t<DH, 2, 2, 32>(qkv, ctx, dctx, lse, delta, dqkv, view, z, st)
-                                                          : span_dq_t<DH, 4, 1, 64>(qkv, ctx, dctx, lse, delta, dqkv, view, z, st);
+  const int rc = span_blocks(z.s, z.heads, z.b) <= 3 * ncu ? span_dq_t<DH, 2, 2, 32>(qkv, ctx, dctx, lse, stats, dqkv, view, z, st)
+                                                          : span_dq_t<DH, 4, 1, 64>(qkv, ctx, dctx, lse, stats, dqkv, view, z, st);
   if (rc != PTDP_OK) return rc;
   const long long blocks = span_blocks(z.s, z.kv_heads, z.b);
   if constexpr (DH > 128) {
-    if (blocks <= 2 * ncu) return span_dkv_t<DH, 2, 2, 32, true>(qkv, dctx, lse, delta, dqkv, view, z, st);
-    return span_dkv_t<DH, 2, 1, 32, true>(qkv, dctx, lse, delta, dqkv, view, z, st);
+    if (blocks <= ncu) return span_dkv_t<DH, 2, 2, 32, true>(qkv, dctx, stats, dqkv, view, z, st);
+    return span_dkv_t<DH, 2, 1, 32, true>(qkv, dctx, stats, dqkv, view, z, st);
+  } else if constexpr (DH > 96) {
+    if (blocks <= 2 * ncu) return span_dkv_t<DH, 2, 2, 64, true>(qkv, dctx, stats, dqkv, view, z, st);
+    if (blocks <= 4 * ncu || z.capped_or_biased()) return span_dkv_t<DH, 2, 1, 64, true>(qkv, dctx, stats, dqkv, view, z, st);
+    return span_dkv_scored_t<DH, 4, 1, 64, false, false>(qkv, dctx, stats, dqkv, view, z, st);
   } else {
-    if (blocks <= 3 * ncu) return span_dkv_t<DH, 2, 2, 32, false>(qkv, dctx, lse, delta, dqkv, view, z, st);
-    return span_dkv_t<DH, 4, 1, 64, false>(qkv, dctx, lse, delta, dqkv, view, z, st);
+    if (blocks <= 4 * ncu) return span_dkv_t<DH, 2, 2, 32, false>(qkv, dctx, stats, dqkv, view, z, st);
+    return span_dkv_t<DH, 4, 1, 64, false>(qkv, dctx, stats, dqkv, view, z, st);
   }
 }
 
@@ -1225,7 +1282,7 @@ int launch_attn_span_fwd(const ptdp_attn_span_cfg* c, const void* qkv, const voi
 }
 
 int launch_attn_span_bwd(const ptdp_attn_span_cfg* c, const void* qkv, const void* spans, const float* slopes, const void* ctx, const float* lse,
-                         const void* dctx, void* dqkv, float* delta, hipStream_t st) {
+                         const void* dctx, void* dqkv, void* workspace, hipStream_t st) {
   const SpanView view = span_view(spans, c->s, c->b);
   const SpanShape z = span_shape(c, slopes);
   Launch L(PTDP_K_ATTN_BWD, 2.0 * span_flops(c), st);
@@ -1233,6 +1290,7 @@ int launch_attn_span_bwd(const ptdp_attn_span_cfg* c, const void* qkv, const voi
   if (c->dtype == PTDP_F32) {
     const int n = (c->s + kF32Rows - 1) / kF32Rows;
     const float *q = (const float*)qkv, *d = (const float*)dctx;
+    float* delta = (float*)workspace;
 #define PTDP_CALL(ND)                                                                                                                                  \
   do {                                                                                                                                                 \
     hipLaunchKernelGGL(attn_span_dq_f32<ND>, dim3(n, c->heads, c->b), dim3(256), 0, st, q, (const float*)ctx, d, lse, delta, (float*)dqkv, view, z, c->dh); \
@@ -1241,7 +1299,7 @@ int launch_attn_span_bwd(const ptdp_attn_span_cfg* c, const void* qkv, const voi
     PTDP_SPAN_F32(c->dh, PTDP_CALL);
 #undef PTDP_CALL
   } else {
-#define PTDP_CALL(D) rc = span_bwd_dh<D>((const bf16_t*)qkv, (const bf16_t*)ctx, (const bf16_t*)dctx, lse, delta, (bf16_t*)dqkv, view, z, st)
+#define PTDP_CALL(D) rc = span_bwd_dh<D>((const bf16_t*)qkv, (const bf16_t*)ctx, (const bf16_t*)dctx, lse, (float2*)workspace, (bf16_t*)dqkv, view, z, st)
     if (c->dh == 32) PTDP_CALL(32);
     else if (c->dh == 64) PTDP_CALL(64);
     else if (c->dh == 96) PTDP_CALL(96);

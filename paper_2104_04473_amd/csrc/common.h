@@ -263,7 +263,8 @@ int launch_attn_spans(int causal, int window, const int32_t* documents, const in
 bool attn_span_fits(const ptdp_attn_span_cfg* cfg);   // a valid one's sizes: what the kernels can address and a launch can number
 int launch_attn_span_fwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, void* ctx, float* lse, hipStream_t st);
 int launch_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, const void* ctx, const float* lse,
-                         const void* dctx, void* dqkv, float* delta, hipStream_t st);
+                         const void* dctx, void* dqkv, void* workspace, hipStream_t st);
+size_t attn_span_stats_bytes(const ptdp_attn_span_cfg* cfg);   // of workspace
 // the gated feed-forward block (gemm.hip, elementwise.hip)
 bool gated_mlp_fits(int dtype, int rows, int width, int inner);
 int launch_gated_act(int gate, const float* z, const float* bias, float* g, int rows, int inner, hipStream_t st);
@@ -272,8 +273,8 @@ int launch_gated_act_bwd(int gate, const float* dg, const float* z, const float*
 int launch_gated_mlp_fwd(int dtype, int gate, const void* u, const void* w, const void* bias, void* z, void* g, int rows, int width, int inner,
                          hipStream_t st);
 size_t gated_mlp_workspace_bytes(int dtype, int rows, int width, int inner);
-int launch_gated_mlp_bwd(int dtype, int gate, const void* dy, const void* w2, const void* z, const void* bias, void* dz, float* dbias, void* workspace,
 void gated_mlp_form_query(int back, int rows, int width, int inner, int* tile_m, int* tile_n, int* groups);
+int launch_gated_mlp_bwd(int dtype, int gate, const void* dy, const void* w2, const void* z, const void* bias, void* dz, float* dbias, void* workspace,
                          int rows, int width, int inner, hipStream_t st);
 
 }  // namespace ptdp

@@ -217,7 +217,8 @@ def test_spans(s, b, causal, window, prefix, mean):
 @pytest.mark.parametrize("dh,heads,kv", [(64, 2, 1), (128, 4, 4), (160, 2, 2), (96, 2, 1)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_hidden_infinities_reach_nothing(dtype, dh, heads, kv, bad):
-    """One document and the padding hold values that are not finite, in q, k, v and dctx: the others' results are the same bits as without."""
+    """One document and the padding hold values that are not finite, in q, k, v and dctx: the others' results are the same bits as without (the bf16
+    dK and dV, whose keys are made again by another road, within their tolerance)."""
     s, b = 150, 2
     r = Rig(dtype, s, b, heads, kv, dh, cap=5.0, bias=True)
     ids = np.repeat(np.array([0] * 45 + [1] * 20 + [2] * 65 + [-1] * 20, dtype=np.int32)[:, None], b, 1)
@@ -231,7 +232,10 @@ def test_hidden_infinities_reach_nothing(dtype, dh, heads, kv, bad):
     r.dctx[gone] = bad
     r.run()
     ok = ~gone
-    assert torch.equal(r.ctx[ok], want[0][ok]) and torch.equal(r.dqkv[ok], want[2][ok])
+    cut = heads * dh if dtype == B.BF16 else r.qkv.shape[2]
+    assert torch.equal(r.ctx[ok], want[0][ok]) and torch.equal(r.dqkv[ok][:, :cut], want[2][ok][:, :cut])
+    if dtype == B.BF16:
+        assert_close(np64(r.dqkv[ok][:, cut:]), np64(want[2][ok][:, cut:]), dtype, "dk, dv", factor=0.5)
     keep = ok[:, 0]
     assert torch.equal(r.lse[:, :, keep], want[1][:, :, keep])
     pad = torch.from_numpy(ids == -1).cuda()
