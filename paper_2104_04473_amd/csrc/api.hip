@@ -1028,7 +1028,7 @@ static int check_span_cfg(const ptdp_attn_span_cfg* c) {
   return attn_dh_supported(c->dtype, c->dh) && attn_span_fits(c) ? PTDP_OK : PTDP_E_UNSUPPORTED;
 }
 size_t ptdp_attn_span_workspace_bytes(const ptdp_attn_span_cfg* cfg) {
-  return check_span_cfg(cfg) == PTDP_OK ? align256(attn_span_stats_bytes(cfg)) : 0;
+  return check_span_cfg(cfg) == PTDP_OK ? align256(attn_span_workspace_bytes(cfg)) : 0;
 }
 int ptdp_attn_span_fwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, void* ctx, float* lse, void* stream) {
   PTDP_TRY(check_span_cfg(cfg));

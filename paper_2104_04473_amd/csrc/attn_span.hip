@@ -607,7 +607,13 @@ struct SpanDkvArgs {
   bf16_t* dqkv;
   SpanView view;
   SpanShape z;
+  int parts;         // of a key block's walk, each a workgroup's
+  float* partial;    // their sums, if there is more than one
 };
+// where a part's sums of one result (dK or dV) of 32 keys begin: registers 4 g .. 4 g + 3 of acc[d] of lane l are the four at 256 (4 d + g) + 4 l
+__device__ __forceinline__ size_t span_partial_at(const SpanShape& z, int part, int j, int kve, int k32, int dk, int dh) {
+  return (((((size_t)part * z.b + j) * z.kv_heads + kve) * ((z.s + 31) / 32) + k32) * 2 + dk) * (32 * (size_t)dh);
+}
 // A key whose dV or dK has a sum that is not finite (`want`: bit 0, bit 1) is made again from the queries that see it and from no others, an
 // element to a lane and query after query: a hidden query's zero weight times what is not finite may have got in.  It reads the kernel's
 // arguments from where the launch left them and is not inlined: kept for it, they would take the kernel's registers.
@@ -678,7 +684,9 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
   const uint32_t lds0 = attn_lds_offset(smem);
   const int s = z.s, b = z.b, nkb = (s + kKeys - 1) / kKeys, group = z.heads / z.kv_heads;
   int kblk, kve, j;   // the first key blocks see the most queries under the causal mask and start first
-  if (!attn_map_tiles<true>(blockIdx.x, nkb, z.kv_heads, b, &kblk, &kve, &j)) return;
+  if (!attn_map_tiles<true>(blockIdx.x, nkb, z.kv_heads * a.parts, b, &kblk, &kve, &j)) return;
+  const int part = kve % a.parts;
+  kve /= a.parts;
   static_assert(!SPLIT || KW == 2);
   // which half of a group takes dK alternates, so that every SIMD gets both
   const bool want_dk = !SPLIT || ((wave / KW) ^ (NP == 2 ? grp : (int)(blockIdx.x >> 8))) & 1;
@@ -715,7 +723,9 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
     qt_first = e < 0 ? 0 : a * kSpanRows / QT;
     qt_end = e < 0 ? 0 : e * kSpanRows / QT + 1;
   }
-  const int nq = qt_end - qt_first, steps = (group * nq + NP - 1) / NP;
+  // tile t of the walk is tile t % nq of head t / nq; a part takes a share of them, one after the other
+  const int nq = qt_end - qt_first, share = (group * nq + a.parts - 1) / a.parts, t_first = part * share;
+  const int t_end = min(group * nq, t_first + share), steps = t_end > t_first ? (t_end - t_first + NP - 1) / NP : 0;
 
   // every wave loads a share of both tiles, or one half of the waves Q and the other dO
   constexpr int kSlices = QT / 16, DW = GW > kSlices ? kSlices : GW;
@@ -723,7 +733,7 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
   TileDma<DH, DW, QT, false> dma_q, dma_do;
   dma_q.init(rs, lane);
   dma_do.init(dors, lane);
-  struct Place { int head, qt; };   // of the group; the tile
+  struct Place { int t, head, qt; };   // of the walk; the head of the group; its tile
   auto settle = [&](Place p) {
     while (p.qt >= qt_end) {
       p.qt -= nq;
@@ -764,11 +774,9 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
   f32x16_t acc[NR][NDT];   // dV and dK, or one of them
 
   {
-    Place at = {0, qt_first + grp};
-    if (nq > 0) at = settle(at);
-    if (nq > 0 && at.head < group) {
-      request(at, 0);
-    }
+    Place at = {t_first + grp, 0, qt_first};
+    if (steps > 0) at = settle({at.t, t_first / nq, qt_first + t_first % nq + grp});
+    if (at.t < t_end) request(at, 0);
 #pragma unroll
     for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -781,12 +789,12 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
       const SpanBounds bnd = bounds_of_tile(at);
       const float bias = SCORED && z.slopes ? ((__attribute__((address_space(4))) const float*)z.slopes)[min(kve * group + head, z.heads - 1)] * z.per_slope : 0.f;
       attn_tiles_ready();
-      const Place then = settle({at.head, at.qt + NP});
-      const bool more = then.head < group;
+      const Place then = settle({at.t + NP, at.head, at.qt + NP});
+      const bool more = then.t < t_end;
       const uint32_t other = stage == 0 ? kStage : 0;
       if (more) request(then, other);
       // (skipped if no key of the wave exists or no query of the tile sees one)
-      if (head < group && key_first < s && bnd.first < key_first + 32 && bnd.last > key_first) {
+      if (at.t < t_end && key_first < s && bnd.first < key_first + 32 && bnd.last > key_first) {
         const FragDirect<QT> fs = f0.at(stage);
         const FragTr<QT> ts = t0.at(stage);
         const char *rows = smem + stage + Geom::kStats, *spans = smem + stage + Geom::kSpans;
@@ -911,6 +919,19 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[x][d][r] += sum[((x * NDT + d) * 16 + r) * 64];
   }
+  if (a.parts > 1) {
+    if (key_first >= s) return;
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+      const bool dk = SPLIT ? want_dk : x == 1;
+      f32x4_t* to = reinterpret_cast<f32x4_t*>(a.partial + span_partial_at(z, part, j, kve, kblk * KW + kw, dk, DH)) + lane;
+#pragma unroll
+      for (int d = 0; d < NDT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) to[(4 * d + g) * 64] = f32x4_t{acc[x][d][4 * g], acc[x][d][4 * g + 1], acc[x][d][4 * g + 2], acc[x][d][4 * g + 3]};
+    }
+    return;
+  }
   bf16_t* out = a.dqkv + (size_t)my_key * rs + j * row + (size_t)(z.heads + kve) * DH;   // dK; dV kv_heads further on
   uint64_t bad[2] = {0, 0};   // keys whose dV, dK has a sum that is not finite
 #pragma unroll
@@ -926,6 +947,40 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
     const int k = __ffsll((unsigned long long)left) - 1;
     span_dkv_again<DH>(*kernargs, key_first + k, kve, j, (int)(bad[0] >> k & 1) | (int)(bad[1] >> k & 1) << 1);
   }
+}
+
+// Adds the parts' sums, in their order: a workgroup has one result of 32 keys, a wave 32 of its columns.
+template <int DH>
+__global__ void __launch_bounds__(DH * 2)
+attn_span_dkv_join_kernel(SpanDkvArgs a) {
+  __shared__ uint32_t bad_keys;
+  const SpanShape& z = a.z;
+  const int nk32 = (z.s + 31) / 32, k32 = blockIdx.x % nk32, pair = blockIdx.x / nk32, kve = pair % z.kv_heads, j = pair / z.kv_heads, dk = blockIdx.y;
+  const int d = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, l31 = lane & 31, my_key = k32 * 32 + l31;
+  if (threadIdx.x == 0) bad_keys = 0;
+  f32x16_t acc[1] = {zero16()};
+  for (int part = 0; part < a.parts; ++part) {
+    const f32x4_t* from = reinterpret_cast<const f32x4_t*>(a.partial + span_partial_at(z, part, j, kve, k32, dk, DH)) + lane;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4_t v = from[(4 * d + g) * 64];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[0][4 * g + i] += v[i];
+    }
+  }
+  __syncthreads();
+  const bool valid = my_key < z.s;
+  const uint64_t m = __ballot(valid && !all_finite(acc));
+  if (m && lane == 0) atomicOr(&bad_keys, (uint32_t)(m | m >> 32));
+  __syncthreads();
+  const uint32_t bad = __builtin_amdgcn_readfirstlane(bad_keys);
+  const size_t row = (size_t)(z.heads + 2 * z.kv_heads) * DH;
+  if (valid && !(bad >> l31 & 1))
+    store_cols<1>(a.dqkv + ((size_t)my_key * z.b + j) * row + (size_t)(z.heads + kve + (dk ? 0 : z.kv_heads)) * DH + d * 32, acc, dk ? z.scale : 1.f, half);
+  if (d > 0) return;
+  const SpanDkvArgs* kernargs = (const SpanDkvArgs*)(const char*)__builtin_amdgcn_kernarg_segment_ptr();
+#pragma unroll 1
+  for (uint32_t left = bad; left; left &= left - 1) span_dkv_again<DH>(*kernargs, k32 * 32 + __ffs(left) - 1, kve, j, 1 + dk);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1178,7 +1233,26 @@ static SpanShape span_shape(const ptdp_attn_span_cfg* c, const float* slopes) {
   const float mul = (capped ? c->cap : c->scale) * kLog2e;
   return {c->s, c->b, c->heads, c->kv_heads, c->scale, c->cap, mul, capped ? 2.f * kLog2e * c->scale / c->cap : 0.f, kLog2e / mul, slopes};
 }
-size_t attn_span_stats_bytes(const ptdp_attn_span_cfg* c) { return (size_t)c->b * c->heads * c->s * sizeof(float2); }   // fp32: D alone
+static long long span_blocks(int s, int heads, int b) { return (long long)((s + 63) / 64) * heads * b; }   // of 64 rows
+// Workgroups that share the walk of a key block whose head serves a group of query heads: as many as there are compute units for
+// (the walk is up to `tiles` tiles of 64 queries long), and up to eight times as many while each is left kSpanShare tiles - fewer are not worth
+// the sums' way through memory.  The workspace holds those sums, so this asks for the chip's units and not for the device's.  dK and dV alone,
+// us, 1 part and the parts taken: 2048 tokens, heads 16 to 2 of 128: 307, 71 (8); 32 to 8 of 64: 115, 58 (4); 1024, 20 to 4 of 160: 120, 45 (4);
+// 256 x 8, 16 to 2 of 64: 34, 20 (4; 24 with 8); 512 x 8, 16 to 4 of 128: 50 (1; 53 with 2).
+constexpr int kSpanUnits = 256, kSpanShare = 32;
+static int span_parts(int s, int heads, int kv_heads, int b) {
+  const int group = heads / kv_heads;
+  const long long blocks = std::max(1ll, span_blocks(s, kv_heads, b)), tiles = (long long)group * ((s + 63) / 64);
+  const long long few = kSpanUnits / blocks, many = std::min(8 * kSpanUnits / blocks, tiles / kSpanShare);
+  return (int)std::max(1ll, std::min((long long)group, std::max(few, many)));
+}
+static size_t span_stats_bytes(int s, int heads, int b) { return ((size_t)b * heads * s * sizeof(float2) + 15) / 16 * 16; }
+size_t attn_span_workspace_bytes(const ptdp_attn_span_cfg* c) {
+  if (c->dtype == PTDP_F32) return (size_t)c->b * c->heads * c->s * sizeof(float);   // D alone
+  const int parts = span_parts(c->s, c->heads, c->kv_heads, c->b);
+  const size_t sums = parts > 1 ? (size_t)parts * c->b * c->kv_heads * ((c->s + 31) / 32) * 64 * c->dh * sizeof(float) : 0;
+  return span_stats_bytes(c->s, c->heads, c->b) + sums;
+}
 // the square's visible part is not known to the host: counted as the causal half
 static double span_flops(const ptdp_attn_span_cfg* c) { return 2.0 * c->b * c->heads * (double)c->s * c->s * c->dh; }
 
@@ -1205,23 +1279,32 @@ static int span_dq_t(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, c
   hipLaunchKernelGGL(kernel, grid, dim3(64 * QW * NP), smem, st, qkv, ctx, dctx, lse, stats, dqkv, view, z);
   return PTDP_OK;
 }
-template <int DH, int KW, int NP, int QT, bool SPLIT, bool SCORED>
-static int span_dkv_scored_t(const bf16_t* qkv, const bf16_t* dctx, const float2* stats, bf16_t* dqkv, const SpanView& view,
-                      const SpanShape& z, hipStream_t st) {
+template <int DH, int KW, int NP, int QT, bool SPLIT, bool SCORED> static int span_dkv_scored_t(const SpanDkvArgs& a, hipStream_t st) {
   using Geom = SpanDkvGeom<DH, KW, NP, QT, SPLIT>;
   static once_flag_t done[kMaxDevices];
   const auto kernel = attn_span_dkv_kernel<DH, KW, NP, QT, SPLIT, SCORED>;
   if (set_dynamic_smem(reinterpret_cast<const void*>(kernel), Geom::kBytes, done) != PTDP_OK) return PTDP_E_HIP;
-  const dim3 grid(attn_grid_levels((z.s + 32 * KW - 1) / (32 * KW), z.kv_heads, z.b));
-  hipLaunchKernelGGL(kernel, grid, dim3(Geom::kThreads * NP), Geom::kBytes, st, SpanDkvArgs{qkv, dctx, stats, dqkv, view, z});
+  const dim3 grid(attn_grid_levels((a.z.s + 32 * KW - 1) / (32 * KW), a.z.kv_heads * a.parts, a.z.b));
+  hipLaunchKernelGGL(kernel, grid, dim3(Geom::kThreads * NP), Geom::kBytes, st, a);
   return PTDP_OK;
 }
-template <int DH, int KW, int NP, int QT, bool SPLIT>
-static int span_dkv_t(const bf16_t* qkv, const bf16_t* dctx, const float2* stats, bf16_t* dqkv, const SpanView& view, const SpanShape& z, hipStream_t st) {
-  return z.capped_or_biased() ? span_dkv_scored_t<DH, KW, NP, QT, SPLIT, true>(qkv, dctx, stats, dqkv, view, z, st)
-                              : span_dkv_scored_t<DH, KW, NP, QT, SPLIT, false>(qkv, dctx, stats, dqkv, view, z, st);
+template <int DH, int KW, int NP, int QT, bool SPLIT> static int span_dkv_t(const SpanDkvArgs& a, hipStream_t st) {
+  return a.z.capped_or_biased() ? span_dkv_scored_t<DH, KW, NP, QT, SPLIT, true>(a, st) : span_dkv_scored_t<DH, KW, NP, QT, SPLIT, false>(a, st);
 }
-static long long span_blocks(int s, int heads, int b) { return (long long)((s + 63) / 64) * heads * b; }   // of 64 rows
+template <int DH> static int span_dkv_dh(const SpanDkvArgs& a, hipStream_t st) {
+  const long long ncu = attn_compute_units(), blocks = span_blocks(a.z.s, a.z.kv_heads * a.parts, a.z.b);
+  if constexpr (DH > 128) {
+    if (blocks <= ncu) return span_dkv_t<DH, 2, 2, 32, true>(a, st);
+    return span_dkv_t<DH, 2, 1, 32, true>(a, st);
+  } else if constexpr (DH > 96) {
+    if (blocks <= 2 * ncu) return span_dkv_t<DH, 2, 2, 64, true>(a, st);
+    if (blocks <= 4 * ncu || a.z.capped_or_biased()) return span_dkv_t<DH, 2, 1, 64, true>(a, st);
+    return span_dkv_scored_t<DH, 4, 1, 64, false, false>(a, st);
+  } else {
+    if (blocks <= 4 * ncu) return span_dkv_t<DH, 2, 2, 32, false>(a, st);
+    return span_dkv_t<DH, 4, 1, 64, false>(a, st);
+  }
+}
 
 template <int DH> static int span_fwd_dh(const bf16_t* qkv, bf16_t* ctx, float* lse, const SpanView& view, const SpanShape& z, hipStream_t st) {
   if (span_blocks(z.s, z.heads, z.b) <= 4 * attn_compute_units()) return span_fwd_t<DH, 2, 2, (DH > 128 ? 32 : 64)>(qkv, ctx, lse, view, z, st);
@@ -1231,21 +1314,15 @@ template <int DH>
 static int span_bwd_dh(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, const float* lse, float2* stats, bf16_t* dqkv, const SpanView& view,
                        const SpanShape& z, hipStream_t st) {
   const long long ncu = attn_compute_units();
-  const int rc = span_blocks(z.s, z.heads, z.b) <= 3 * ncu ? span_dq_t<DH, 2, 2, 32>(qkv, ctx, dctx, lse, stats, dqkv, view, z, st)
+  int rc = span_blocks(z.s, z.heads, z.b) <= 3 * ncu ? span_dq_t<DH, 2, 2, 32>(qkv, ctx, dctx, lse, stats, dqkv, view, z, st)
                                                           : span_dq_t<DH, 4, 1, 64>(qkv, ctx, dctx, lse, stats, dqkv, view, z, st);
   if (rc != PTDP_OK) return rc;
-  const long long blocks = span_blocks(z.s, z.kv_heads, z.b);
-  if constexpr (DH > 128) {
-    if (blocks <= ncu) return span_dkv_t<DH, 2, 2, 32, true>(qkv, dctx, stats, dqkv, view, z, st);
-    return span_dkv_t<DH, 2, 1, 32, true>(qkv, dctx, stats, dqkv, view, z, st);
-  } else if constexpr (DH > 96) {
-    if (blocks <= 2 * ncu) return span_dkv_t<DH, 2, 2, 64, true>(qkv, dctx, stats, dqkv, view, z, st);
-    if (blocks <= 4 * ncu || z.capped_or_biased()) return span_dkv_t<DH, 2, 1, 64, true>(qkv, dctx, stats, dqkv, view, z, st);
-    return span_dkv_scored_t<DH, 4, 1, 64, false, false>(qkv, dctx, stats, dqkv, view, z, st);
-  } else {
-    if (blocks <= 4 * ncu) return span_dkv_t<DH, 2, 2, 32, false>(qkv, dctx, stats, dqkv, view, z, st);
-    return span_dkv_t<DH, 4, 1, 64, false>(qkv, dctx, stats, dqkv, view, z, st);
-  }
+  SpanDkvArgs a = {qkv, dctx, stats, dqkv, view, z, span_parts(z.s, z.heads, z.kv_heads, z.b), nullptr};
+  a.partial = reinterpret_cast<float*>(reinterpret_cast<char*>(stats) + span_stats_bytes(z.s, z.heads, z.b));
+  rc = span_dkv_dh<DH>(a, st);
+  if (rc != PTDP_OK || a.parts == 1) return rc;
+  hipLaunchKernelGGL(attn_span_dkv_join_kernel<DH>, dim3((z.s + 31) / 32 * z.kv_heads * z.b, 2), dim3(DH * 2), 0, st, a);
+  return PTDP_OK;
 }
 
 // steps of 16 dh, rounded up to one of the built forms

@@ -264,7 +264,7 @@ bool attn_span_fits(const ptdp_attn_span_cfg* cfg);   // a valid one's sizes: wh
 int launch_attn_span_fwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, void* ctx, float* lse, hipStream_t st);
 int launch_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, const void* ctx, const float* lse,
                          const void* dctx, void* dqkv, void* workspace, hipStream_t st);
-size_t attn_span_stats_bytes(const ptdp_attn_span_cfg* cfg);   // of workspace
+size_t attn_span_workspace_bytes(const ptdp_attn_span_cfg* cfg);
 // the gated feed-forward block (gemm.hip, elementwise.hip)
 bool gated_mlp_fits(int dtype, int rows, int width, int inner);
 int launch_gated_act(int gate, const float* z, const float* bias, float* g, int rows, int inner, hipStream_t st);
