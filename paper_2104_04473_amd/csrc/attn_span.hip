@@ -591,15 +591,22 @@ template <int QT> __device__ __forceinline__ void span_load_rows(const void* fro
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds + i * 256), "v"(i * 256 + lane * 4), "s"(r) : "memory", "m0");
 }
 
-// dK, dV of 32 KW keys of a key/value head: the queries of the group's heads that may see them, head after head, stream through two LDS
-// stages of QT queries, with their statistics (lse, D) and spans, all of it straight from memory.  Nothing of the next tile passes through
-// vector registers: both results, K and V leave none over.
-// SPLIT: KW waves compute S, dP and dK and KW waves S and dV (heads of 160: both results do not fit two waves' registers).
+// dK, dV of 32 KW keys of a key/value head: the queries of the group's heads that may see them, head after head, stream through LDS stages
+// of QT queries, with their statistics (lse, D) and spans, all of it straight from memory.  Nothing of the next tile passes through vector
+// registers: both results, K and V leave none over.
+// SPLIT: KW waves keep K and V and make P and dS of a tile, KW waves keep both results and add the tile before it up; the weights go from one
+// to the other through LDS as the fragments they are, and three stages hold the tiles.  A SIMD has one wave of each kind, so that exponentials
+// run beside products, and no score is made twice.  Heads of 128 and 160, whose results and operands together fill more than a wave's registers;
+// dK/dV alone, us, against two halves of which each makes the scores and one result: 4096 x 20 x 160: 243 and 295; capped with 4 key/value heads:
+// 300 and 487; 16384 in documents, 8 x 128 on 2: 637 and 784.  Smaller heads: one wave does it all (2048 x 32 x 64: 50, split 58).
 template <int DH, int KW, int NP, int QT, bool SPLIT> struct SpanDkvGeom {
   static constexpr int kWaves = SPLIT ? 2 * KW : KW, kThreads = 64 * kWaves;   // of a group
   static constexpr int kTile = QT * DH * 2, kStats = 2 * kTile, kSpans = kStats + 8 * QT, kStage = kSpans + 8 * QT;
+  static constexpr int kStages = SPLIT ? 3 : 2, kWeights = kStages * kStage, kWave = QT / 32 * 4096;   // P and dS of a wave's tile
+  static constexpr int kGroup = kWeights + (SPLIT ? 2 * KW * kWave : 0);
   static constexpr int kSums = NP > 1 ? KW * 2 * (DH / 2) * 64 * (int)sizeof(float) : 0;
-  static constexpr int kBytes = NP * 2 * kStage > kSums ? NP * 2 * kStage : kSums;
+  static constexpr int kBytes = NP * kGroup > kSums ? NP * kGroup : kSums;
+  static_assert(kBytes <= 160 * 1024);
 };
 struct SpanDkvArgs {
   const bf16_t *qkv, *dctx;
@@ -667,7 +674,7 @@ template <int DH> __device__ __attribute__((noinline)) void span_dkv_again(const
     if (want & 1) to[(size_t)z.kv_heads * DH + 64 * i + lane] = f32_to_bf16(dv[i]);
   }
 }
-// SCORED: there may be a cap or a bias (without that code heads of 160 fit their registers).
+// SCORED: there may be a cap or a bias.
 template <int DH, int KW, int NP, int QT, bool SPLIT, bool SCORED>
 __global__ void __launch_bounds__(64 * KW * (SPLIT ? 2 : 1) * NP, 2)
 attn_span_dkv_kernel(SpanDkvArgs a) {
@@ -675,21 +682,19 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
   const SpanShape& z = a.z;
   using Geom = SpanDkvGeom<DH, KW, NP, QT, SPLIT>;
   constexpr int NKK = DH / 16, NDT = DH / 32, kKeys = 32 * KW, SUBS = QT / 32, GW = Geom::kWaves, kTile = Geom::kTile, kStage = Geom::kStage;
-  constexpr int NR = SPLIT ? 1 : 2;   // results of a wave
   extern __shared__ __attribute__((aligned(1024))) char smem_all[];
   const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = NP == 1 ? 0 : wave_all / GW, wave = wave_all % GW;
   const int kw = wave % KW;
   static_assert(GW > 1);
-  char* smem = smem_all + grp * 2 * kStage;
+  char* smem = smem_all + grp * Geom::kGroup;
   const uint32_t lds0 = attn_lds_offset(smem);
   const int s = z.s, b = z.b, nkb = (s + kKeys - 1) / kKeys, group = z.heads / z.kv_heads;
   int kblk, kve, j;   // the first key blocks see the most queries under the causal mask and start first
   if (!attn_map_tiles<true>(blockIdx.x, nkb, z.kv_heads * a.parts, b, &kblk, &kve, &j)) return;
   const int part = kve % a.parts;
   kve /= a.parts;
-  static_assert(!SPLIT || KW == 2);
-  // which half of a group takes dK alternates, so that every SIMD gets both
-  const bool want_dk = !SPLIT || ((wave / KW) ^ (NP == 2 ? grp : (int)(blockIdx.x >> 8))) & 1;
+  // (which half makes the weights alternates where it takes that to give every SIMD both)
+  const bool sums_only = SPLIT && ((wave / KW) ^ (KW == 4 ? 0 : NP == 2 ? grp : (int)(blockIdx.x >> 8))) & 1;
   const int lane = threadIdx.x & 63, half = lane >> 5, l31 = lane & 31;
   const size_t row = (size_t)(z.heads + 2 * z.kv_heads) * DH, rs = b * row, orow = (size_t)z.heads * DH, dors = b * orow;
   const bf16_t* sample = a.qkv + j * row;
@@ -727,9 +732,8 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
   const int nq = qt_end - qt_first, share = (group * nq + a.parts - 1) / a.parts, t_first = part * share;
   const int t_end = min(group * nq, t_first + share), steps = t_end > t_first ? (t_end - t_first + NP - 1) / NP : 0;
 
-  // every wave loads a share of both tiles, or one half of the waves Q and the other dO
+  // every wave loads a share of both tiles, or one half's first waves Q and the other's dO
   constexpr int kSlices = QT / 16, DW = GW > kSlices ? kSlices : GW;
-  static_assert(GW <= 2 * kSlices);
   TileDma<DH, DW, QT, false> dma_q, dma_do;
   dma_q.init(rs, lane);
   dma_do.init(dors, lane);
@@ -743,11 +747,11 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
   };
   auto request = [&](Place p, uint32_t at) {
     if (GW == DW || wave < DW) dma_q.issue(qb + (size_t)p.head * DH, p.qt * QT, s, lds0 + at, wave % DW);
-    if (GW == DW || wave >= DW) dma_do.issue(dob + (size_t)p.head * DH, p.qt * QT, s, lds0 + at + kTile, wave % DW);
+    if (GW == DW || (wave >= GW / 2 && wave < GW / 2 + DW)) dma_do.issue(dob + (size_t)p.head * DH, p.qt * QT, s, lds0 + at + kTile, wave % DW);
     // eight bytes a query, zeros past the end
     const int q = p.qt * QT, bytes = min(QT, s - q) * 8;
-    if (wave == 0) span_load_rows<QT>(a.stats + stat0 + (size_t)p.head * s + q, bytes, lds0 + at + Geom::kStats, lane);
-    if (wave == 1 && view.range) span_load_rows<QT>(view.range + (size_t)j * s + q, bytes, lds0 + at + Geom::kSpans, lane);
+    if (wave == GW - 1) span_load_rows<QT>(a.stats + stat0 + (size_t)p.head * s + q, bytes, lds0 + at + Geom::kStats, lane);
+    if (wave == GW - 2 && view.range) span_load_rows<QT>(view.range + (size_t)j * s + q, bytes, lds0 + at + Geom::kSpans, lane);
   };
   // the tile's bounds and bias, from scalar loads: they are a tile's to wait for, not a lane's
   typedef __attribute__((address_space(4))) const int scalar_int_t;
@@ -761,127 +765,143 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
     }
     return x;
   };
-  bf16x8_t kf[NKK], vf[NKK];
-#pragma unroll
-  for (int kk = 0; kk < NKK; ++kk) {
-    kf[kk] = frag_global(kb + (size_t)min(my_key, s - 1) * rs, valid, kk, half);
-    vf[kk] = frag_global(vb + (size_t)min(my_key, s - 1) * rs, valid, kk, half);
-  }
   FragDirect<QT> f0;
   FragTr<QT> t0;
   f0.init(lds0, l31, half);
   t0.init(lds0, lane);
-  f32x16_t acc[NR][NDT];   // dV and dK, or one of them
+  f32x16_t acc[2][NDT];   // dV and dK
 
-  {
+  // the walk of a wave that makes the weights (P and dS), that adds up dV and dK, or that does both
+  auto walk = [&](auto weights, auto sums) {
+    constexpr bool WEIGHTS = decltype(weights)::value, SUMS = decltype(sums)::value;
+    bf16x8_t kf[NKK], vf[NKK];
+    if constexpr (WEIGHTS) {
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        kf[kk] = frag_global(kb + (size_t)min(my_key, s - 1) * rs, valid, kk, half);
+        vf[kk] = frag_global(vb + (size_t)min(my_key, s - 1) * rs, valid, kk, half);
+      }
+    }
+    if constexpr (SUMS) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int d = 0; d < NDT; ++d) acc[r][d] = zero16();
+    }
     Place at = {t_first + grp, 0, qt_first};
     if (steps > 0) at = settle({at.t, t_first / nq, qt_first + t_first % nq + grp});
     if (at.t < t_end) request(at, 0);
-#pragma unroll
-    for (int r = 0; r < NR; ++r)
-#pragma unroll
-      for (int d = 0; d < NDT; ++d) acc[r][d] = zero16();
-    uint32_t stage = 0;
-    // all groups take the same number of steps (the barriers are the workgroup's); a group without a tile idles
+    uint32_t stage = 0, before = 0, slot = Geom::kWeights + kw * Geom::kWave;
+    bool had = false;   // the tile before was one to be done
+    // all groups take the same number of steps (the barriers are the workgroup's); a group without a tile idles.  Where the work is split
+    // the sums are a tile behind the weights.
 #pragma unroll 1
-    for (int step = 0; step < steps; ++step) {
+    for (int step = 0; step < (SPLIT && steps > 0 ? steps + 1 : steps); ++step) {
       const int q0 = at.qt * QT, head = at.head;
       const SpanBounds bnd = bounds_of_tile(at);
-      const float bias = SCORED && z.slopes ? ((__attribute__((address_space(4))) const float*)z.slopes)[min(kve * group + head, z.heads - 1)] * z.per_slope : 0.f;
+      const float bias = WEIGHTS && SCORED && z.slopes ? ((__attribute__((address_space(4))) const float*)z.slopes)[min(kve * group + head, z.heads - 1)] * z.per_slope : 0.f;
       attn_tiles_ready();
       const Place then = settle({at.t + NP, at.head, at.qt + NP});
-      const bool more = then.t < t_end;
-      const uint32_t other = stage == 0 ? kStage : 0;
-      if (more) request(then, other);
+      const uint32_t other = stage == (Geom::kStages - 1) * kStage ? 0 : stage + kStage;
+      if (then.t < t_end) request(then, other);
       // (skipped if no key of the wave exists or no query of the tile sees one)
-      if (at.t < t_end && key_first < s && bnd.first < key_first + 32 && bnd.last > key_first) {
+      const bool here = at.t < t_end && key_first < s && bnd.first < key_first + 32 && bnd.last > key_first;
+      if (WEIGHTS ? here : had) {
         const FragDirect<QT> fs = f0.at(stage);
-        const FragTr<QT> ts = t0.at(stage);
+        const FragTr<QT> ts = t0.at(SPLIT ? before : stage);
         const char *rows = smem + stage + Geom::kStats, *spans = smem + stage + Geom::kSpans;
         const bool full = bnd.inner_lo <= key_first && bnd.inner_hi >= key_first + 32;
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-          f32x16_t sacc = zero16(), dp = zero16();
-          if (!SPLIT || want_dk) {
+          bf16x8_t pf[2], dsf[2];
+          // P and dS on their way from one wave to the other: four fragments, each 16 bytes of a lane
+          bf16x8_t* way = reinterpret_cast<bf16x8_t*>(smem + slot + sub * 4096) + lane;
+          if constexpr (WEIGHTS) {
+            f32x16_t sacc = zero16(), dp = zero16();
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk) {
               sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs.get(sub, kk), kf[kk], sacc, 0, 0, 0);
               dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs.get(sub, kk, kTile), vf[kk], dp, 0, 0, 0);
             }
             sched_reads_ahead<2 * NKK, 1>();
-          } else {
+            __builtin_amdgcn_sched_barrier(0);
+            const float ahead = (float)(my_key - q0 - sub * 32 - 4 * half);
+            if (SCORED && z.slopes && !z.capped()) {
 #pragma unroll
-            for (int kk = 0; kk < NKK; ++kk) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs.get(sub, kk), kf[kk], sacc, 0, 0, 0);
-            sched_reads_ahead<NKK, 1>();
-          }
-          __builtin_amdgcn_sched_barrier(0);
-          const float ahead = (float)(my_key - q0 - sub * 32 - 4 * half);
-          if (SCORED && z.slopes && !z.capped()) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sacc[r] = fmaf(-bias, fabsf(ahead - (float)acc_row(r)), sacc[r]);
-          }
-          if (SCORED && z.capped()) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const char* four = rows + (sub * 32 + 8 * g + 4 * half) * 8;   // lse and D of four consecutive queries
-              const f32x4_t two[2] = {*reinterpret_cast<const f32x4_t*>(four), *reinterpret_cast<const f32x4_t*>(four + 16)};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int r = 4 * g + i;
-                const float th = z.tanh(sacc[r]), p = __builtin_amdgcn_exp2f(fmaf(-bias, fabsf(ahead - (float)acc_row(r)), th) * z.mul - two[i >> 1][2 * (i & 1)]);
-                sacc[r] = p;
-                dp[r] = p * (dp[r] - two[i >> 1][2 * (i & 1) + 1]) * fmaf(-th, th, 1.f);
-              }
+              for (int r = 0; r < 16; ++r) sacc[r] = fmaf(-bias, fabsf(ahead - (float)acc_row(r)), sacc[r]);
             }
-          } else {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const char* four = rows + (sub * 32 + 8 * g + 4 * half) * 8;
-              const f32x4_t two[2] = {*reinterpret_cast<const f32x4_t*>(four), *reinterpret_cast<const f32x4_t*>(four + 16)};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int r = 4 * g + i;
-                const float p = __builtin_amdgcn_exp2f(sacc[r] * z.mul - two[i >> 1][2 * (i & 1)]);
-                sacc[r] = p;
-                dp[r] = p * (dp[r] - two[i >> 1][2 * (i & 1) + 1]);
-              }
-            }
-          }
-          if (!full) {
-            typedef int i32x4_t __attribute__((ext_vector_type(4)));
-            if (view.range) {
+            if (SCORED && z.capped()) {
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
-                const char* four = spans + (sub * 32 + 8 * g + 4 * half) * 8;
-                const i32x4_t two[2] = {*reinterpret_cast<const i32x4_t*>(four), *reinterpret_cast<const i32x4_t*>(four + 16)};
+                const char* four = rows + (sub * 32 + 8 * g + 4 * half) * 8;   // lse and D of four consecutive queries
+                const f32x4_t two[2] = {*reinterpret_cast<const f32x4_t*>(four), *reinterpret_cast<const f32x4_t*>(four + 16)};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {   // (an empty span, {kNoKey, 0}, has no key either: no key is as far from kNoKey as 0 is)
-                  const int lo = two[i >> 1][2 * (i & 1)], hi = two[i >> 1][2 * (i & 1) + 1];
-                  const bool seen = (uint32_t)(my_key - lo) < (uint32_t)(hi - lo);
-                  sacc[4 * g + i] = seen ? sacc[4 * g + i] : 0.f;
-                  dp[4 * g + i] = seen ? dp[4 * g + i] : 0.f;
+                for (int i = 0; i < 4; ++i) {
+                  const int r = 4 * g + i;
+                  const float th = z.tanh(sacc[r]), p = __builtin_amdgcn_exp2f(fmaf(-bias, fabsf(ahead - (float)acc_row(r)), th) * z.mul - two[i >> 1][2 * (i & 1)]);
+                  sacc[r] = p;
+                  dp[r] = p * (dp[r] - two[i >> 1][2 * (i & 1) + 1]) * fmaf(-th, th, 1.f);
                 }
               }
             } else {
-              const int before = my_key - q0 - sub * 32 - 4 * half;   // local queries below it precede my_key
 #pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                sacc[r] = acc_row(r) < before ? 0.f : sacc[r];
-                dp[r] = acc_row(r) < before ? 0.f : dp[r];
+              for (int g = 0; g < 4; ++g) {
+                const char* four = rows + (sub * 32 + 8 * g + 4 * half) * 8;
+                const f32x4_t two[2] = {*reinterpret_cast<const f32x4_t*>(four), *reinterpret_cast<const f32x4_t*>(four + 16)};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int r = 4 * g + i;
+                  const float p = __builtin_amdgcn_exp2f(sacc[r] * z.mul - two[i >> 1][2 * (i & 1)]);
+                  sacc[r] = p;
+                  dp[r] = p * (dp[r] - two[i >> 1][2 * (i & 1) + 1]);
+                }
               }
             }
+            if (!full) {
+              typedef int i32x4_t __attribute__((ext_vector_type(4)));
+              if (view.range) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                  const char* four = spans + (sub * 32 + 8 * g + 4 * half) * 8;
+                  const i32x4_t two[2] = {*reinterpret_cast<const i32x4_t*>(four), *reinterpret_cast<const i32x4_t*>(four + 16)};
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {   // (an empty span, {kNoKey, 0}, has no key either: no key is as far from kNoKey as 0 is)
+                    const int lo = two[i >> 1][2 * (i & 1)], hi = two[i >> 1][2 * (i & 1) + 1];
+                    const bool seen = (uint32_t)(my_key - lo) < (uint32_t)(hi - lo);
+                    sacc[4 * g + i] = seen ? sacc[4 * g + i] : 0.f;
+                    dp[4 * g + i] = seen ? dp[4 * g + i] : 0.f;
+                  }
+                }
+              } else {
+                const int before = my_key - q0 - sub * 32 - 4 * half;   // local queries below it precede my_key
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                  sacc[r] = acc_row(r) < before ? 0.f : sacc[r];
+                  dp[r] = acc_row(r) < before ? 0.f : dp[r];
+                }
+              }
+            }
+            pf[0] = pack_frag(sacc, 0);
+            pf[1] = pack_frag(sacc, 1);
+            dsf[0] = pack_frag(dp, 0);
+            dsf[1] = pack_frag(dp, 1);
           }
-          const bf16x8_t pf[2] = {pack_frag(sacc, 0), pack_frag(sacc, 1)}, dsf[2] = {pack_frag(dp, 0), pack_frag(dp, 1)};
-          if constexpr (SPLIT) {
-            // Q^T or dO^T; P or dS
-            const uint32_t tile = want_dk ? 0 : kTile;
-            const FragTr<QT> tw{ts.lo + tile, ts.hi + tile};
+          if constexpr (SPLIT && WEIGHTS) {
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
+            for (int ks = 0; ks < 2; ++ks) {
+              way[ks * 64] = pf[ks];
+              way[(2 + ks) * 64] = dsf[ks];
+            }
+          }
+          if constexpr (SUMS) {
+            if constexpr (SPLIT) {
 #pragma unroll
-              for (int d = 0; d < NDT; ++d) acc[0][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tw.get(d, sub, ks), want_dk ? dsf[ks] : pf[ks], acc[0][d], 0, 0, 0);
-            sched_reads_ahead<2 * NDT, 2>();
-          } else {
+              for (int ks = 0; ks < 2; ++ks) {
+                pf[ks] = way[ks * 64];
+                dsf[ks] = way[(2 + ks) * 64];
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -895,16 +915,37 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
         }
       }
       at = then;
+      before = stage;
       stage = other;
+      had = here;
+      if (WEIGHTS || step > 0) slot = slot < Geom::kWeights + KW * Geom::kWave ? slot + KW * Geom::kWave : slot - KW * Geom::kWave;
     }
+    if constexpr (SUMS) {   // whole accumulators up to here: the loop is not to carry the pieces that the stores want
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int d = 0; d < NDT; ++d) asm volatile("" : "+v"(acc[r][d]));
+    }
+  };
+  if constexpr (!SPLIT) walk(std::true_type{}, std::true_type{});
+  if constexpr (SPLIT) {
+    if (!sums_only) {
+      walk(std::true_type{}, std::false_type{});
+      if constexpr (NP > 1) {   // (the barriers below)
+        __syncthreads();
+        __syncthreads();
+      }
+      return;
+    }
+    walk(std::false_type{}, std::true_type{});
   }
   if constexpr (NP > 1) {
-    // the second group's sums join the first's: register r of lane l of the wave with keys kw (and one result) at sum[..][r][l]
-    float* sum = reinterpret_cast<float*>(smem_all) + (SPLIT ? (want_dk ? KW : 0) + kw : 2 * kw) * (NDT * 16 * 64) + lane;
+    // the second group's sums join the first's: register r of lane l of the wave with keys kw at sum[..][r][l]
+    float* sum = reinterpret_cast<float*>(smem_all) + 2 * kw * (NDT * 16 * 64) + lane;
     __syncthreads();   // every wave is done with the tiles
     if (grp == 1) {
 #pragma unroll
-      for (int x = 0; x < NR; ++x)
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int d = 0; d < NDT; ++d)
 #pragma unroll
@@ -913,7 +954,7 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
     __syncthreads();
     if (grp == 1) return;
 #pragma unroll
-    for (int x = 0; x < NR; ++x)
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int d = 0; d < NDT; ++d)
 #pragma unroll
@@ -922,9 +963,8 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
   if (a.parts > 1) {
     if (key_first >= s) return;
 #pragma unroll
-    for (int x = 0; x < NR; ++x) {
-      const bool dk = SPLIT ? want_dk : x == 1;
-      f32x4_t* to = reinterpret_cast<f32x4_t*>(a.partial + span_partial_at(z, part, j, kve, kblk * KW + kw, dk, DH)) + lane;
+    for (int x = 0; x < 2; ++x) {
+      f32x4_t* to = reinterpret_cast<f32x4_t*>(a.partial + span_partial_at(z, part, j, kve, kblk * KW + kw, x, DH)) + lane;
 #pragma unroll
       for (int d = 0; d < NDT; ++d)
 #pragma unroll
@@ -935,11 +975,10 @@ attn_span_dkv_kernel(SpanDkvArgs a) {
   bf16_t* out = a.dqkv + (size_t)my_key * rs + j * row + (size_t)(z.heads + kve) * DH;   // dK; dV kv_heads further on
   uint64_t bad[2] = {0, 0};   // keys whose dV, dK has a sum that is not finite
 #pragma unroll
-  for (int x = 0; x < NR; ++x) {
-    const bool dk = SPLIT ? want_dk : x == 1;
-    const uint64_t m = __ballot(valid && !all_finite(acc[x])), either = (m | m >> 32) & 0xffffffffu;
-    if (valid && !(either >> l31 & 1)) store_cols<NDT>(out + (dk ? 0 : (size_t)z.kv_heads * DH), acc[x], dk ? z.scale : 1.f, half);
-    bad[dk ? 1 : 0] = either;
+  for (int x = 0; x < 2; ++x) {
+    const uint64_t m = __ballot(valid && !all_finite(acc[x]));
+    bad[x] = (m | m >> 32) & 0xffffffffu;
+    if (valid && !(bad[x] >> l31 & 1)) store_cols<NDT>(out + (x == 1 ? 0 : (size_t)z.kv_heads * DH), acc[x], x == 1 ? z.scale : 1.f, half);
   }
   const SpanDkvArgs* kernargs = (const SpanDkvArgs*)(const char*)__builtin_amdgcn_kernarg_segment_ptr();   // (only a kernel knows the place)
 #pragma unroll 1
@@ -1291,17 +1330,17 @@ template <int DH, int KW, int NP, int QT, bool SPLIT, bool SCORED> static int sp
 template <int DH, int KW, int NP, int QT, bool SPLIT> static int span_dkv_t(const SpanDkvArgs& a, hipStream_t st) {
   return a.z.capped_or_biased() ? span_dkv_scored_t<DH, KW, NP, QT, SPLIT, true>(a, st) : span_dkv_scored_t<DH, KW, NP, QT, SPLIT, false>(a, st);
 }
+// Few key blocks: two groups of waves to each, which take its tiles in turn (2048 tokens, 16 heads of 128, 512 blocks: 62 us, 128 keys to a workgroup
+// 76).  Many: 128 keys to a workgroup (4 x 2048: 183 and 235), unless rows are short (8 x 512: 64 keys 42, 128 keys 54; 16 x 512, heads of 32: two groups
+// 27, 128 keys 34).
 template <int DH> static int span_dkv_dh(const SpanDkvArgs& a, hipStream_t st) {
   const long long ncu = attn_compute_units(), blocks = span_blocks(a.z.s, a.z.kv_heads * a.parts, a.z.b);
-  if constexpr (DH > 128) {
-    if (blocks <= ncu) return span_dkv_t<DH, 2, 2, 32, true>(a, st);
-    return span_dkv_t<DH, 2, 1, 32, true>(a, st);
-  } else if constexpr (DH > 96) {
-    if (blocks <= 2 * ncu) return span_dkv_t<DH, 2, 2, 64, true>(a, st);
-    if (blocks <= 4 * ncu || a.z.capped_or_biased()) return span_dkv_t<DH, 2, 1, 64, true>(a, st);
-    return span_dkv_scored_t<DH, 4, 1, 64, false, false>(a, st);
+  if constexpr (DH > 96) {
+    if (blocks <= 2 * ncu) return span_dkv_t<DH, 2, 2, 32, true>(a, st);
+    if (a.z.s <= 1024) return span_dkv_t<DH, 2, 1, 32, true>(a, st);
+    return span_dkv_t<DH, 4, 1, 32, true>(a, st);
   } else {
-    if (blocks <= 4 * ncu) return span_dkv_t<DH, 2, 2, 32, false>(a, st);
+    if (blocks <= 4 * ncu || a.z.s <= 1024) return span_dkv_t<DH, 2, 2, 32, false>(a, st);
     return span_dkv_t<DH, 4, 1, 64, false>(a, st);
   }
 }
