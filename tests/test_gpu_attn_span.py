@@ -192,6 +192,30 @@ def test_long(s, b, heads, kv, dh, options):
     assert all(torch.equal(a, t) for a, t in zip(first, (r.ctx, r.lse, r.dqkv)))
 
 
+FORMS = [  # the other ways that dK and dV are cut up: short rows of many, long rows of many, walks of shared heads in parts
+    (300, 8, 16, 16, 128, {}),
+    (300, 8, 16, 16, 160, dict(cap=20.0, docs=70)),
+    (1100, 2, 16, 16, 128, dict(docs=300)),
+    (1100, 2, 16, 16, 160, dict(bias=True)),
+    (1100, 4, 16, 16, 32, {}),
+    (1100, 4, 16, 16, 96, dict(cap=15.0, prefix=True)),
+    (6000, 1, 8, 2, 128, dict(docs=1500)),
+    (5000, 1, 16, 4, 64, dict(window=700)),
+    (700, 1, 8, 1, 32, dict(docs=9, bias=True)),   # parts without a tile
+]
+
+
+@gpu
+@pytest.mark.parametrize("s,b,heads,kv,dh,options", FORMS)
+def test_forms_of_key_gradients(s, b, heads, kv, dh, options):
+    r = Rig(B.BF16, s, b, heads, kv, dh, **options)
+    r.run()
+    r.compare(r.dense())
+    first = r.dqkv.clone()
+    r.run()
+    assert torch.equal(first, r.dqkv)
+
+
 @gpu
 @pytest.mark.parametrize("s,b", [(1, 1), (255, 2), (256, 1), (257, 3), (1000, 2), (5000, 1), (9001, 2)])
 @pytest.mark.parametrize("causal,window,prefix", [(True, 0, False), (True, 0, True), (False, 0, False), (True, 37, False), (False, 300, False)])
