@@ -100,6 +100,14 @@ def main():
                [lambda i=i: B.ptdp_bias_gelu_bwd(B.BF16, B.GELU_ERF, gs[i].data_ptr(), zs[i].data_ptr(), b1.data_ptr(),
                                                  gs[i].data_ptr(), db1.data_ptr(), scratch.data_ptr(), T, fp, sh) for i in range(n)])
         del zs, gs
+        turns = torch.tensor(B.rotary_turns(dh), dtype=torch.float64, device=dev)
+        n = sets(3 * hp, 2)
+        xs = [rnd(T, 3 * hp) for _ in range(n)]; us = [torch.empty(T, 3 * hp, dtype=bf, device=dev) for _ in range(n)]
+        for name, call in (("rotary_fwd", B.ptdp_rotary_fwd), ("rotary_bwd", B.ptdp_rotary_bwd)):
+            report(name, T * 3 * hp * 4, "GB/s",
+                   [lambda i=i: call(B.BF16, B.ROTARY_HALVES, xs[i].data_ptr(), None, turns.data_ptr(), us[i].data_ptr(), w["s"], w["b"], heads, heads,
+                                     dh, dh, 1.0, sh) for i in range(n)])
+        del xs, us
 
     if args.only == "all":
         # ---- GEMMs of one layer ----------------------------------------------------------------------------
@@ -119,6 +127,17 @@ def main():
                    [lambda: B.ptdp_gemm(B.BF16, B.GEMM_TN, a.data_ptr(), dy.data_ptr(), dw.data_ptr(), None, K, N, T, 1, 1,
                                         ws.data_ptr(), ws.numel(), sh)])
             del a, wgt, c, dy, dx, dw
+        # ---- gated feed-forward block: its two fused products -------------------------------------------------
+        u = rnd(T, h); wgt = rnd(h, 2 * fp, scale=0.02); z = torch.empty(T, 2 * fp, dtype=bf, device=dev); g = torch.empty(T, fp, dtype=bf, device=dev)
+        report("gated feed-forward forward [%d x 2 x %d x %d]" % (T, fp, h), 4.0 * T * fp * h, "TFLOP/s",
+               [lambda: B.ptdp_gated_mlp_fwd(B.BF16, B.GATE_SILU, u.data_ptr(), wgt.data_ptr(), None, z.data_ptr(), g.data_ptr(), T, h, fp, sh)])
+        del wgt
+        w2 = rnd(fp, h, scale=0.02); dz = torch.empty_like(z)
+        gws = torch.empty(B.ptdp_gated_mlp_workspace_bytes(B.BF16, T, h, fp), dtype=torch.uint8, device=dev)
+        report("gated feed-forward backward [%d x %d x %d]" % (T, fp, h), 2.0 * T * fp * h, "TFLOP/s",
+               [lambda: B.ptdp_gated_mlp_bwd(B.BF16, B.GATE_SILU, u.data_ptr(), w2.data_ptr(), z.data_ptr(), None, dz.data_ptr(), None, gws.data_ptr(),
+                                             T, h, fp, sh)])
+        del u, z, g, w2, dz
 
     if args.only == "elementwise":
         return
@@ -133,6 +152,18 @@ def main():
     report("attention backward (full-square FLOP count)", 2 * fl, "TFLOP/s",
            [lambda: B.ptdp_attn_bwd(B.BF16, qkv.data_ptr(), ctx.data_ptr(), lse.data_ptr(), dctx.data_ptr(), dqkv.data_ptr(),
                                     delta.data_ptr(), w["s"], w["b"], heads, dh, sh)])
+    # under spans: the causal mask, and documents of a quarter of the length with capped scores
+    ids = (torch.arange(w["s"], device=dev, dtype=torch.int32) // (w["s"] // 4))[:, None].repeat(1, w["b"]).contiguous()
+    spans = torch.empty(B.ptdp_attn_spans_bytes(w["s"], w["b"]), dtype=torch.uint8, device=dev)
+    report("spans of documents", 12.0 * T, "GB/s", [lambda: B.ptdp_attn_spans(1, 0, ids.data_ptr(), None, spans.data_ptr(), w["s"], w["b"], sh)])
+    for name, at, cap in (("causal", None, 0.0), ("four documents, capped", spans.data_ptr(), 50.0)):
+        cfg = B.make_span_cfg(w["s"], w["b"], heads, heads, dh, cap=cap)
+        sws = torch.empty(B.ptdp_attn_span_workspace_bytes(C.byref(cfg)), dtype=torch.uint8, device=dev)
+        report("attention under spans forward, %s (full-square FLOP count)" % name, fl, "TFLOP/s",
+               [lambda: B.ptdp_attn_span_fwd(C.byref(cfg), qkv.data_ptr(), at, None, ctx.data_ptr(), lse.data_ptr(), sh)])
+        report("attention under spans backward, %s (full-square FLOP count)" % name, 2 * fl, "TFLOP/s",
+               [lambda: B.ptdp_attn_span_bwd(C.byref(cfg), qkv.data_ptr(), at, None, ctx.data_ptr(), lse.data_ptr(), dctx.data_ptr(), dqkv.data_ptr(),
+                                             sws.data_ptr(), sh)])
 
 
 if __name__ == "__main__":
