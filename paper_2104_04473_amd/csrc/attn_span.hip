@@ -1225,10 +1225,10 @@ attn_span_dq_f32(const float* __restrict__ qkv, const float* __restrict__ ctx, c
 template <int ND>
 __global__ void __launch_bounds__(256)
 attn_span_dkv_f32(const float* __restrict__ qkv, const float* __restrict__ dctx, const float* __restrict__ lse, const float* __restrict__ delta,
-                  float* __restrict__ dqkv, SpanView view, SpanShape z, int dh) {
+                  float* __restrict__ dqkv, SpanView view, SpanShape z, int dh, int parts, float* __restrict__ partial) {
   __shared__ f32x4_t part[3 * ND * 64];
   const int kve = blockIdx.y, j = blockIdx.z, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int s = z.s, b = z.b, k0 = blockIdx.x * kF32Rows, my_key = k0 + c, kr = min(my_key, s - 1), group = z.heads / z.kv_heads;
+  const int mine_of = blockIdx.x % parts, s = z.s, b = z.b, k0 = blockIdx.x / parts * kF32Rows, my_key = k0 + c, kr = min(my_key, s - 1), group = z.heads / z.kv_heads;
   const size_t row = (size_t)(z.heads + 2 * z.kv_heads) * dh, rs = b * row, orow = (size_t)z.heads * dh, dors = b * orow;
   const float* sample = qkv + j * row;
   const float *kb = sample + (size_t)(z.heads + kve) * dh, *vb = kb + (size_t)z.kv_heads * dh;
@@ -1262,7 +1262,7 @@ attn_span_dkv_f32(const float* __restrict__ qkv, const float* __restrict__ dctx,
 #pragma unroll
   for (int t = 0; t < ND; ++t) dk[t] = dv[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-  for (int at = wave; at < group * nq; at += 4) {
+  for (int at = wave + 4 * mine_of; at < group * nq; at += 4 * parts) {
     const int head = kve * group + at / nq, q0 = (qt_first + at % nq) * kF32Rows, qc = min(q0 + c, s - 1);
     const F32Rule rule(z, head);
     const float *qb = sample + (size_t)head * dh, *dob = dctx + j * orow + (size_t)head * dh;
@@ -1291,10 +1291,22 @@ attn_span_dkv_f32(const float* __restrict__ qkv, const float* __restrict__ dctx,
     f32_accumulate<ND>(dv, p, dob, dors, q0, s, dh, some, vis, lane);
     f32_accumulate<ND>(dk, ds, qb, rs, q0, s, dh, some, vis, lane);
   }
-  float* out = dqkv + (size_t)my_key * rs + j * row + (size_t)(z.heads + kve) * dh;
+  // (a part's sums: [s, b, 2 kv_heads dh])
+  float* out = parts > 1 ? partial + (((size_t)mine_of * s + my_key) * b + j) * 2 * z.kv_heads * dh + (size_t)kve * dh
+                         : dqkv + (size_t)my_key * rs + j * row + (size_t)(z.heads + kve) * dh;
   const bool mine = f32_join<ND>(dk, part, wave, lane);
   if (mine && my_key < s) f32_store<ND>(out, dk, g, dh);
   if (f32_join<ND>(dv, part, wave, lane) && my_key < s) f32_store<ND>(out + (size_t)z.kv_heads * dh, dv, g, dh);
+}
+
+// Adds the parts' sums in their order, four elements to a thread.
+__global__ void __launch_bounds__(256) attn_span_dkv_join_f32(const float* __restrict__ partial, float* __restrict__ dqkv, SpanShape z, int dh, int parts) {
+  const size_t width = 2 * (size_t)z.kv_heads * dh, n = (size_t)z.s * z.b * width, i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  f32x4_t sum = *reinterpret_cast<const f32x4_t*>(partial + i);
+  for (int p = 1; p < parts; ++p) sum += *reinterpret_cast<const f32x4_t*>(partial + p * n + i);
+  const size_t r = i / width;
+  *reinterpret_cast<f32x4_t*>(dqkv + r * (width + (size_t)z.heads * dh) + (size_t)z.heads * dh + (i - r * width)) = sum;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1324,9 +1336,21 @@ static int span_parts(int s, int heads, int kv_heads, int b) {
   const long long few = kSpanUnits / blocks, many = std::min(8 * kSpanUnits / blocks, tiles / kSpanShare);
   return (int)std::max(1ll, std::min((long long)group, std::max(few, many)));
 }
+// The same for fp32, whose workgroups of 16 keys take a compute unit or half of one (3 x 187 tokens, 16 heads to 4 of 160, forward and backward: 300 us
+// in one part, 240 in three).
+constexpr int kSpanUnitsF32 = 2 * kSpanUnits, kSpanShareF32 = 2;   // tiles of 16 queries left to each of four waves
+static int span_parts_f32(int s, int heads, int kv_heads, int b) {
+  const int group = heads / kv_heads;
+  const long long n = (s + kF32Rows - 1) / kF32Rows, blocks = std::max(1ll, n * kv_heads * b);
+  return (int)std::max(1ll, std::min({(long long)group, kSpanUnitsF32 / blocks, n * group / (4 * kSpanShareF32)}));
+}
+static size_t span_delta_bytes(int s, int heads, int b) { return ((size_t)b * heads * s * sizeof(float) + 15) / 16 * 16; }
 static size_t span_stats_bytes(int s, int heads, int b) { return ((size_t)b * heads * s * sizeof(float2) + 15) / 16 * 16; }
 size_t attn_span_workspace_bytes(const ptdp_attn_span_cfg* c) {
-  if (c->dtype == PTDP_F32) return (size_t)c->b * c->heads * c->s * sizeof(float);   // D alone
+  if (c->dtype == PTDP_F32) {   // D, and the parts' sums
+    const int parts = span_parts_f32(c->s, c->heads, c->kv_heads, c->b);
+    return span_delta_bytes(c->s, c->heads, c->b) + (parts > 1 ? (size_t)parts * c->s * c->b * 2 * c->kv_heads * c->dh * sizeof(float) : 0);
+  }
   const int parts = span_parts(c->s, c->heads, c->kv_heads, c->b);
   const size_t sums = parts > 1 ? (size_t)parts * c->b * c->kv_heads * ((c->s + 31) / 32) * 64 * c->dh * sizeof(float) : 0;
   return span_stats_bytes(c->s, c->heads, c->b) + sums;
@@ -1448,14 +1472,19 @@ int launch_attn_span_bwd(const ptdp_attn_span_cfg* c, const void* qkv, const voi
   if (c->dtype == PTDP_F32) {
     const int n = (c->s + kF32Rows - 1) / kF32Rows;
     const float *q = (const float*)qkv, *d = (const float*)dctx;
-    float* delta = (float*)workspace;
+    float *delta = (float*)workspace, *partial = (float*)((char*)workspace + span_delta_bytes(c->s, c->heads, c->b));
+    const int parts = span_parts_f32(c->s, c->heads, c->kv_heads, c->b);
 #define PTDP_CALL(ND)                                                                                                                                  \
   do {                                                                                                                                                 \
     hipLaunchKernelGGL(attn_span_dq_f32<ND>, dim3(n, c->heads, c->b), dim3(256), 0, st, q, (const float*)ctx, d, lse, delta, (float*)dqkv, view, z, c->dh); \
-    hipLaunchKernelGGL(attn_span_dkv_f32<ND>, dim3(n, c->kv_heads, c->b), dim3(256), 0, st, q, d, lse, (const float*)delta, (float*)dqkv, view, z, c->dh);   \
+    hipLaunchKernelGGL(attn_span_dkv_f32<ND>, dim3(n * parts, c->kv_heads, c->b), dim3(256), 0, st, q, d, lse, (const float*)delta, (float*)dqkv, view, z,  \
+                       c->dh, parts, partial);                                                                                                         \
   } while (0)
     PTDP_SPAN_F32(c->dh, PTDP_CALL);
 #undef PTDP_CALL
+    if (parts > 1)
+      hipLaunchKernelGGL(attn_span_dkv_join_f32, dim3((unsigned)(((size_t)c->s * c->b * c->kv_heads * c->dh / 2 + 255) / 256)), dim3(256), 0, st, partial,
+                         (float*)dqkv, z, c->dh, parts);
   } else {
 #define PTDP_CALL(D) rc = span_bwd_dh<D>((const bf16_t*)qkv, (const bf16_t*)ctx, (const bf16_t*)dctx, lse, (float2*)workspace, (bf16_t*)dqkv, view, z, st)
     if (c->dh == 32) PTDP_CALL(32);
