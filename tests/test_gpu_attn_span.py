@@ -371,3 +371,13 @@ def test_refusals():
         assert spans(*bad) == B.E_INVALID_ARG, bad
     assert spans(1, 0, None, None, p, 1, 70000) == B.E_UNSUPPORTED and B.ptdp_attn_spans_bytes(-1, 1) == 0 and B.ptdp_attn_spans_bytes(1, 70000) == 0
     assert B.ptdp_attn_spans_bytes(33, 2) == 33 * 2 * 8 + 2 * 2 * 16
+
+
+@pytest.mark.parametrize("dtype", [B.BF16, B.F32])
+def test_workspace_bytes(dtype):
+    """Statistics of every query, and sums of dK and dV where few key blocks of shared heads are walked in parts: at most one set for each query head."""
+    for s, b, heads, kv, dh in ((0, 1, 4, 2, 64), (1, 0, 4, 2, 64), (1, 1, 4, 1, 64), (33, 2, 8, 8, 128), (2048, 1, 16, 2, 128), (16384, 1, 8, 2, 128)):
+        n = B.ptdp_attn_span_workspace_bytes(C.byref(B.make_span_cfg(s, b, heads, kv, dh, dtype)))
+        rows = (s + 31) // 32 * 32 * b * heads
+        least = s * b * heads * (8 if dtype == B.BF16 else 4)
+        assert least <= n <= rows * 8 + (heads > kv) * rows * 2 * dh * 4 + 256, (s, b, heads, kv, dh, n)
