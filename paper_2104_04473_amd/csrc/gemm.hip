@@ -2683,7 +2683,7 @@ int launch_gemm_gelu_bwd(int dtype, int gelu_mode, const void* dg, const void* w
 // Gated feed-forward block: z[M, 2 F] = u[M, K] w[K, 2 F] and g = f(z_gate + b) (z_up + b) in one kernel, and dg = dy w2^T with what makes dz of it.
 // The forward's tile is the plain kernels' with half of its columns from the gate's and half from the up projection's half of w, so that
 // the same lane ends up with both and nothing is read back; what bounds it is what bounds the product.  Forward, 2048 x 2 x 6144 x 12288: 473 to
-// 488 us, 1.27 to 1.31 PFLOP/s; 8192 x 2 x 8192 x 2048: 427 us, 1.29.  Backward, 2048 x 12800 x 25600: 1024 us, 1.31; 1998 x 5504 x 2048, 172 tiles:
+// 488 us, 1.27 to 1.31 PFLOP/s; 8192 x 2 x 8192 x 2048: 427 us, 1.29.  Backward, 2048 x 12800 x 25600: 1024 us, 1.31; 1998 x 5504 x 2048, 232 tiles:
 // 66 us, 0.68; 8192 x 8192 x 2048, where z and dz, 537 MB, take 109 us by themselves: 290 us.
 // ------------------------------------------------------------------------------------------------
 template <bool TB>
