@@ -508,7 +508,8 @@ typedef struct ptdp_attn_span_cfg {
  * A query with an empty span gets zeros and lse = -inf.  What a query does not see reaches none of its results, infinities and NaN included. */
 int ptdp_attn_span_fwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, void* ctx, float* lse, void* stream);
 /* dqkv (all of it; not qkv's buffer) from dctx; K and V gradients are summed over the heads that share them, without atomics.  workspace: dev,
- * ptdp_attn_span_workspace_bytes(cfg) bytes (0 on an invalid cfg). */
+ * ptdp_attn_span_workspace_bytes(cfg) bytes (0 on an invalid cfg; where few key/value heads are shared, sums of dK and dV are in it too, at most 8 dh
+ * bytes for each token and query head). */
 int ptdp_attn_span_bwd(const ptdp_attn_span_cfg* cfg, const void* qkv, const void* spans, const float* slopes, const void* ctx, const float* lse,
                        const void* dctx, void* dqkv, void* workspace, void* stream);
 size_t ptdp_attn_span_workspace_bytes(const ptdp_attn_span_cfg* cfg);
